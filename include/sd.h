@@ -40,7 +40,9 @@ typedef enum {
   SD_EHIP   = 5    /* a HIP call failed */
 } sd_status;
 
-typedef enum { SD_F32 = 0, SD_BF16 = 1 } sd_dtype;
+typedef enum { SD_F32 = 0, SD_BF16 = 1,
+               SD_E4M3 = 2   /* 8-bit floats with 4 exponent and 3 mantissa bits (no infinities): key-value caches only */
+} sd_dtype;
 
 enum { SD_ARCH_GPT = 0, SD_ARCH_T5DEC = 1, SD_ARCH_GQA = 2 };
 enum { SD_MAX_GAMMA = 15 };       /* a sequence contributes at most SD_MAX_GAMMA+1 rows to a forward */
@@ -418,6 +420,84 @@ sd_status sd_spec_sample_static(const float* p_logits, const float* q_logits, co
                                 const float* r, const float* s, int32_t rows, int32_t gamma,
                                 int32_t vocab, float temperature, const sd_sampling* opt,
                                 int32_t* out_n, int32_t* out_t, float* beta, void* stream);
+
+/*
+ * A paged key-value cache apart from a model: for callers whose models are their own (as
+ * sd_spec_sample is), one layer of the layout that the models here use.  sd_kv_append writes rows of keys and
+ * values, sd_kv_attention lets a few query rows of every sequence (one token, or the gamma+1 rows
+ * of a verify forward) attend over it, sd_kv_read gives rows back.
+ *   pool       : dev, [n_pages][2: K, V][n_kv_heads][page_size][d_head] of dtype
+ *                (SD_BF16, or SD_E4M3: one byte), 16-byte aligned
+ *   exps       : dev, [n_pages][2][n_kv_heads][page_size] bytes, 16-byte aligned (SD_E4M3; else ignored)
+ *   page_table : dev, [n_seq][table_stride]: position p of sequence s lies in page
+ *                page_table[s][p / page_size], slot p % page_size.  Entries that no position in use
+ *                needs may be anything; an entry outside 0..n_pages-1 has no page behind it.
+ *   page_size  : power of two, >= 16;  d_head: 32, 64 or 128
+ * SD_E4M3 keeps a row x of d_head values (one position, one head, K or V) as codes c and a byte e:
+ * x = c 2^(e-127), where 2^(e-127) is the smallest power of two in 2^-111..2^120 with which the row's largest
+ * finite magnitude is at most 448; codes are x 2^(127-e) rounded to the nearest, ties to even
+ * (relative error at most 2^-4 down to 2^-15 of that magnitude), beyond 240 * 2^120 = 1.875 * 2^127 that number.
+ * NaN and infinities are kept as NaN.
+ * All calls are asynchronous on `stream`, allocate nothing and may be captured into a graph.
+ * The struct (host) is read during the call.  Every pointer belongs to the device that is current.
+ * Reasons of refusals: sd_last_error(NULL).
+ */
+typedef struct {
+  void*          pool;
+  uint8_t*       exps;
+  const int32_t* page_table;
+  int32_t        dtype;            /* SD_BF16 or SD_E4M3 */
+  int32_t        n_pages, n_seq, table_stride, page_size, n_kv_heads, d_head;
+} sd_kv_cache;
+
+/* Rows of keys and values outside the cache: head h of row i at k + i * k_row_stride + h * k_head_stride (in
+ * elements, multiples of 8; d_head consecutive elements, 16-byte aligned pointers). */
+typedef struct {
+  void *k, *v;                     /* dev; sd_kv_append reads them, sd_kv_read writes them */
+  int64_t k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+  int32_t dtype;                   /* SD_F32 or SD_BF16 */
+} sd_kv_rows;
+
+/*
+ * Write rows into the cache / read rows of it.
+ *   seq, pos : dev, [rows] int32: row i is position pos[i] of sequence seq[i].  seq == NULL: every sequence has
+ *              rows / n_seq rows, one after the other.  pos == NULL: positions 0, 1, .. of each sequence.
+ *   rows     : 0 is allowed and does nothing
+ * A row whose position is negative or beyond the table, whose sequence is none of the n_seq, or whose table entry has no
+ * page is not written, and read as zeros.  Two rows of one append at the same place: what the
+ * cache then holds there is unspecified.  In an SD_BF16 cache values are rounded to bf16.
+ */
+sd_status sd_kv_append(const sd_kv_cache* cache, const sd_kv_rows* rows_in, const int32_t* seq, const int32_t* pos,
+                       int32_t rows, void* stream);
+sd_status sd_kv_read(const sd_kv_cache* cache, const sd_kv_rows* rows_out, const int32_t* seq, const int32_t* pos,
+                     int32_t rows, void* stream);
+
+/*
+ * Attention over the cache, `rows` query rows per sequence (row r of sequence s is row i = s * rows + r):
+ *   out = sum_j p_j v_j / sum_j p_j,  p_j = e^(scale q.k_j),  lse = ln sum_j p_j,  over the positions j = 0..pos[i].
+ * Query head h reads kv head h / (n_heads / n_kv_heads).  Sums and softmax are fp32; the cache's values and the
+ * queries enter exactly, probabilities to 2^-17 (SD_BF16) or 2^-24 (SD_F32).
+ *   q        : dev, SD_F32 or SD_BF16 (`dtype`, also out's), head h of row i at i * q_row_stride + h *
+ *              q_head_stride (elements, multiples of 8), 16-byte aligned
+ *   pos      : dev, [n_seq * rows] int32, the last position that a row sees (for appended rows: their own);
+ *              negative: none.  Every row has its own: sequences with fewer rows are padded with -1.
+ *   max_len  : no row sees a position >= max_len, whatever pos says; 1..SD_KV_MAX_LEN.  The
+ *              work is cut up by it: pass what the contexts can reach rather than the table's size.
+ *   out      : dev, [n_seq * rows][n_heads][d_head];  lse: dev, [n_seq * rows][n_heads] fp32, or NULL
+ *   scratch  : dev, sd_kv_attention_scratch_bytes() bytes, 16-byte aligned, zeroed once by the caller before its first
+ *              use; calls of any shape that fit it may follow one another on a stream.  Calls
+ *              that overlap in time (and graphs that do) need one each.
+ * A row that sees nothing gets out = 0 and lse = -infinity.  Positions whose table entry has no page are not seen.
+ * What lies in unused slots, or at positions a row does not see, never reaches it, NaN and infinities included; a row that sees
+ * a V that is not finite has NaN (or an infinity) in that feature; |V| beyond 2^100 may overflow the running sums.  A sequence's result depends on its own rows, on max_len and on how the call is
+ * cut up (n_seq, rows and heads decide), never on other sequences' contents; the same call gives the same bits.
+ * n_seq * ceil(rows * n_heads / n_kv_heads / 32) * n_kv_heads is at most SD_KV_MAX_GROUPS (SD_ERANGE otherwise).
+ */
+enum { SD_KV_MAX_LEN = 524288, SD_KV_MAX_GROUPS = 65536 };
+size_t    sd_kv_attention_scratch_bytes(const sd_kv_cache* cache, int32_t n_heads, int32_t rows, int32_t max_len);
+sd_status sd_kv_attention(const sd_kv_cache* cache, const void* q, int64_t q_row_stride, int64_t q_head_stride,
+                          int32_t dtype, const int32_t* pos, int32_t n_heads, int32_t rows, int32_t max_len,
+                          float scale, void* out, float* lse, void* scratch, size_t scratch_bytes, void* stream);
 
 #ifdef __cplusplus
 }

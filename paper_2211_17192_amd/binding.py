@@ -21,7 +21,7 @@ if not os.path.exists(LIB_PATH):
 lib = C.CDLL(LIB_PATH)
 
 SD_OK, SD_EINVAL, SD_ESTATE, SD_ERANGE, SD_ENOMEM, SD_EHIP = range(6)
-SD_F32, SD_BF16 = 0, 1
+SD_F32, SD_BF16, SD_E4M3 = 0, 1, 2
 SD_MAX_GAMMA = 15
 SD_FLAG_GRAPH, SD_FLAG_PROFILE, SD_FLAG_BETA, SD_FLAG_SCATTER_PAGES, SD_FLAG_SEPARATE_CROSS_Q = 1, 2, 4, 8, 16
 STATUS_NAMES = ["SD_OK", "SD_EINVAL", "SD_ESTATE", "SD_ERANGE", "SD_ENOMEM", "SD_EHIP"]
@@ -139,6 +139,180 @@ def spec_sample_static(p_logits, q_logits, x, r, s, temperature: float, out_n, o
     if st != SD_OK:
         raise SdError(st, (lib.sd_last_error(None) or b"").decode())
     return out_n, out_t
+
+
+# --------------------------------------------------------------------------
+# the paged key-value cache apart from a model
+# --------------------------------------------------------------------------
+class _KvCache(C.Structure):
+    _fields_ = [("pool", C.c_void_p), ("exps", C.c_void_p), ("page_table", C.c_void_p)] + \
+               [(n, C.c_int32) for n in ("dtype", "n_pages", "n_seq", "table_stride", "page_size", "n_kv_heads", "d_head")]
+
+
+class _KvRows(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p)] + \
+               [(n, C.c_int64) for n in ("k_row_stride", "k_head_stride", "v_row_stride", "v_head_stride")] + [("dtype", C.c_int32)]
+
+
+for _f in (lib.sd_kv_append, lib.sd_kv_read):
+    _f.restype = C.c_int
+    _f.argtypes = [C.POINTER(_KvCache), C.POINTER(_KvRows), C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]
+lib.sd_kv_attention_scratch_bytes.restype = C.c_size_t
+lib.sd_kv_attention_scratch_bytes.argtypes = [C.POINTER(_KvCache), C.c_int32, C.c_int32, C.c_int32]
+lib.sd_kv_attention.restype = C.c_int
+lib.sd_kv_attention.argtypes = [C.POINTER(_KvCache), C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_int32, C.c_int32,
+                                C.c_int32, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+SD_KV_MAX_LEN = 524288
+_ROW_TYPES = {torch.float32: SD_F32, torch.bfloat16: SD_BF16}
+
+
+def _refuse(msg):
+    raise SdError(SD_EINVAL, msg)
+
+
+class KvCache:
+    """One layer's paged key-value cache (sd_kv_cache) on the current device, in 8 bits ("e4m3": codes with a power of two per
+    row) or bf16.  page_table: cuda int32 [n_seq, entries].  pool ([n_pages, 2, n_kv_heads, page_size, d_head], uint8 or
+    bfloat16) and exps ([n_pages, 2, n_kv_heads, page_size] uint8) are made here unless given.  The calls are
+    asynchronous on the current stream; the tensors are kept alive here.
+
+    pos is a cuda int32 tensor with the position of every row, [n_seq, rows] (or any shape of that many entries where seq, the rows'
+    sequences, is given too); -1 is a row that is absent."""
+
+    def __init__(self, page_table, n_pages: int, n_kv_heads: int, d_head: int, page_size: int = 16, dtype: str = "e4m3",
+                 pool=None, exps=None):
+        if dtype not in ("e4m3", "bf16"):
+            _refuse("dtype must be 'e4m3' or 'bf16'")
+        if not page_table.is_cuda or page_table.dim() != 2 or page_table.dtype != torch.int32 or not page_table.is_contiguous():
+            _refuse("page_table must be a contiguous cuda int32 tensor [n_seq, entries]")
+        self._device = dev = page_table.device
+        shape = (int(n_pages), 2, int(n_kv_heads), int(page_size), int(d_head))
+        if min(shape) < 1:
+            _refuse("non-positive size of the cache")
+        el = torch.uint8 if dtype == "e4m3" else torch.bfloat16
+        self.pool = torch.zeros(shape, dtype=el, device=dev) if pool is None else pool
+        self.exps = None
+        if dtype == "e4m3":
+            self.exps = torch.full(shape[:4], 127, dtype=torch.uint8, device=dev) if exps is None else exps
+        for name, t, sh, dt in (("pool", self.pool, shape, el), ("exps", self.exps, shape[:4], torch.uint8)):
+            if t is not None and (t.device != dev or tuple(t.shape) != sh or t.dtype != dt or not t.is_contiguous()):
+                _refuse(f"{name} must be a contiguous {dt} tensor {list(sh)} on {dev}")
+        self.page_table = page_table
+        self.dtype, self.n_seq, self.n_kv_heads, self.d_head = dtype, page_table.shape[0], shape[2], shape[4]
+        self.capacity = page_table.shape[1] * shape[3]      # positions of a sequence
+        self._c = _KvCache(self.pool.data_ptr(), _ptr(self.exps), page_table.data_ptr(), SD_E4M3 if dtype == "e4m3" else SD_BF16,
+                           shape[0], self.n_seq, page_table.shape[1], shape[3], shape[2], shape[4])
+        self._ref = C.byref(self._c)
+
+    @staticmethod
+    def _check(st):
+        if st != SD_OK:
+            raise SdError(st, (lib.sd_last_error(None) or b"").decode())
+
+    def _here(self, *tensors):
+        if self._device.index != torch.cuda.current_device():
+            _refuse(f"the cache lies on {self._device}, which is not the current device")
+        for t in tensors:
+            if t is not None and t.device != self._device:
+                _refuse(f"a tensor lies on {t.device}, the cache on {self._device}")
+
+    def _indices(self, pos, seq):
+        """Number of rows that pos (and seq) describe, after their checks."""
+        for name, t in (("pos", pos), ("seq", seq)):
+            if t is not None and (t.dtype != torch.int32 or not t.is_contiguous()):
+                _refuse(f"{name} must be a contiguous int32 tensor")
+        n = pos.numel()
+        if seq is not None:
+            if seq.numel() != n:
+                _refuse("seq and pos must have an entry per row")
+        elif pos.dim() < 2 or pos.shape[0] != self.n_seq:
+            _refuse("pos must be [n_seq, rows] where seq is not given")
+        return n
+
+    def _rows(self, k, v, n):
+        """sd_kv_rows of k and v: any leading dimensions with n entries in all and one distance between them, then [n_kv_heads, d_head]."""
+        if k.dtype not in _ROW_TYPES or k.dtype != v.dtype:
+            _refuse("k and v must be float32 or bfloat16, both the same")
+        strides = []
+        for t in (k, v):
+            if t.dim() < 3 or t.shape[-2:] != (self.n_kv_heads, self.d_head) or t.numel() != n * self.n_kv_heads * self.d_head:
+                _refuse(f"k and v must be [.., {self.n_kv_heads}, {self.d_head}] with a row for each of the {n} positions")
+            strides += _row_strides(t)
+        return _KvRows(k.data_ptr(), v.data_ptr(), *strides, _ROW_TYPES[k.dtype])
+
+    def append(self, k, v, pos, seq=None):
+        """sd_kv_append: rows k, v [n_seq, rows, n_kv_heads, d_head] (with seq: [rows, ..]), float32 or bfloat16, to the
+        positions pos.  k and v may be views with strides (parts of one projection's output)."""
+        self._here(k, v, pos, seq)
+        n = self._indices(pos, seq)
+        if n:
+            self._check(lib.sd_kv_append(self._ref, C.byref(self._rows(k, v, n)), _ptr(seq), pos.data_ptr(), n, _stream()))
+
+    def read(self, pos, seq=None, dtype=torch.bfloat16, k_out=None, v_out=None):
+        """sd_kv_read: (k, v) [*pos.shape, n_kv_heads, d_head] at the positions pos; zeros where there is none."""
+        if k_out is None:
+            k_out = torch.empty(*pos.shape, self.n_kv_heads, self.d_head, dtype=dtype, device=self._device)
+        if v_out is None:
+            v_out = torch.empty(*pos.shape, self.n_kv_heads, self.d_head, dtype=dtype, device=self._device)
+        self._here(k_out, v_out, pos, seq)
+        n = self._indices(pos, seq)
+        if n:
+            self._check(lib.sd_kv_read(self._ref, C.byref(self._rows(k_out, v_out, n)), _ptr(seq), pos.data_ptr(), n, _stream()))
+        return k_out, v_out
+
+    def attention_scratch(self, n_heads: int, rows: int, max_len: int = None) -> torch.Tensor:
+        """Scratch of attention calls with `rows` rows a sequence; reusable by calls on one stream."""
+        n = lib.sd_kv_attention_scratch_bytes(self._ref, int(n_heads), int(rows), int(max_len or min(self.capacity, SD_KV_MAX_LEN)))
+        if n == 0:
+            raise SdError(SD_EINVAL, (lib.sd_last_error(None) or b"").decode())
+        return torch.zeros(n, dtype=torch.uint8, device=self._device)
+
+    def attention(self, q, pos, scale=None, max_len=None, out=None, lse=None, scratch=None):
+        """sd_kv_attention: q [n_seq, rows, n_heads, d_head] (float32 or bfloat16) attends to the positions 0 .. pos[n_seq, rows];
+        returns out, of q's shape and type.  scale: 1 / sqrt(d_head) by default.  max_len: a bound of the
+        contexts, the table's capacity by default.  lse: a float32 tensor [n_seq, rows, n_heads] that receives the logarithms of the sums."""
+        if q.dim() != 4 or q.shape[0] != self.n_seq or q.shape[3] != self.d_head or q.dtype not in _ROW_TYPES:
+            _refuse(f"q must be a float32 or bfloat16 tensor [{self.n_seq}, rows, n_heads, {self.d_head}]")
+        S, R, H, D = q.shape
+        if pos.shape != (S, R) or pos.dtype != torch.int32 or not pos.is_contiguous():
+            _refuse("pos must be a contiguous int32 tensor [n_seq, rows]")
+        if out is None:
+            out = torch.empty(S, R, H, D, dtype=q.dtype, device=self._device)
+        elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
+            _refuse("out must be a contiguous tensor of q's shape and type")
+        if lse is not None and (lse.shape != (S, R, H) or lse.dtype != torch.float32 or not lse.is_contiguous()):
+            _refuse("lse must be a contiguous float32 tensor [n_seq, rows, n_heads]")
+        if q.numel() == 0:
+            return out
+        if max_len is None:
+            max_len = min(self.capacity, SD_KV_MAX_LEN)
+        if scratch is None:
+            scratch = self.attention_scratch(H, R, max_len)
+        elif not scratch.is_contiguous():
+            _refuse("scratch must be contiguous")
+        self._here(q, pos, out, lse, scratch)
+        row, head = _row_strides(q)
+        self._check(lib.sd_kv_attention(self._ref, q.data_ptr(), row, head, _ROW_TYPES[q.dtype], pos.data_ptr(), H, R, int(max_len),
+                                        D ** -0.5 if scale is None else float(scale), out.data_ptr(), _ptr(lse), scratch.data_ptr(),
+                                        scratch.numel() * scratch.element_size(), _stream()))
+        return out
+
+
+def _row_strides(t):
+    """Distances from row to row and from head to head of t [.., heads, d_head]; refuses what has no one distance between rows."""
+    if t.stride(-1) != 1:
+        _refuse("the last dimension must be contiguous")
+    row = None
+    for d in range(t.dim() - 3, -1, -1):                  # leading dimensions, innermost first: each must continue the next
+        if t.shape[d] == 1:
+            continue
+        if row is None:
+            row, reach = t.stride(d), t.stride(d) * t.shape[d]
+        elif t.stride(d) != reach:
+            _refuse("the rows must lie at one distance")
+        else:
+            reach *= t.shape[d]
+    return [row or 0, t.stride(-2) if t.shape[-2] > 1 else 0]
 
 
 # --------------------------------------------------------------------------

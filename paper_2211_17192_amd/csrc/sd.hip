@@ -18,6 +18,7 @@
 #include "../../include/sd.h"
 #include "kernels_attn.h"
 #include "kernels_gemm.h"
+#include "kernels_kv.h"
 #include "kernels_misc.h"
 #include "kernels_prompt.h"
 #include "kernels_sample.h"
@@ -1899,3 +1900,4 @@ extern "C" sd_status sd_get_stats(sd_ctx* c, sd_stats* out) {
 }
 
 #include "spec_sample_api.hip"
+#include "kv_api.hip"
