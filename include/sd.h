@@ -491,7 +491,7 @@ sd_status sd_kv_read(const sd_kv_cache* cache, const sd_kv_rows* rows_out, const
  * What lies in unused slots, or at positions a row does not see, never reaches it, NaN and infinities included; a row that sees
  * a V that is not finite has NaN (or an infinity) in that feature; |V| beyond 2^100 may overflow the running sums.  A sequence's result depends on its own rows, on max_len and on how the call is
  * cut up (n_seq, rows and heads decide), never on other sequences' contents; the same call gives the same bits.
- * n_seq * ceil(rows * n_heads / n_kv_heads / 32) * n_kv_heads is at most SD_KV_MAX_GROUPS (SD_ERANGE otherwise).
+ * n_seq * ceil(rows * n_heads / n_kv_heads / 16) * n_kv_heads is at most SD_KV_MAX_GROUPS (SD_ERANGE otherwise).
  */
 enum { SD_KV_MAX_LEN = 524288, SD_KV_MAX_GROUPS = 65536 };
 size_t    sd_kv_attention_scratch_bytes(const sd_kv_cache* cache, int32_t n_heads, int32_t rows, int32_t max_len);

@@ -185,7 +185,8 @@ class KvCache:
             _refuse("dtype must be 'e4m3' or 'bf16'")
         if not page_table.is_cuda or page_table.dim() != 2 or page_table.dtype != torch.int32 or not page_table.is_contiguous():
             _refuse("page_table must be a contiguous cuda int32 tensor [n_seq, entries]")
-        self._device = dev = page_table.device
+        self._device, self._index = page_table.device, page_table.get_device()
+        dev = self._device
         shape = (int(n_pages), 2, int(n_kv_heads), int(page_size), int(d_head))
         if min(shape) < 1:
             _refuse("non-positive size of the cache")
@@ -200,53 +201,56 @@ class KvCache:
         self.page_table = page_table
         self.dtype, self.n_seq, self.n_kv_heads, self.d_head = dtype, page_table.shape[0], shape[2], shape[4]
         self.capacity = page_table.shape[1] * shape[3]      # positions of a sequence
+        self._row_size = shape[2] * shape[4]
         self._c = _KvCache(self.pool.data_ptr(), _ptr(self.exps), page_table.data_ptr(), SD_E4M3 if dtype == "e4m3" else SD_BF16,
                            shape[0], self.n_seq, page_table.shape[1], shape[3], shape[2], shape[4])
         self._ref = C.byref(self._c)
 
-    @staticmethod
-    def _check(st):
+    def _check(self, st):
         if st != SD_OK:
             raise SdError(st, (lib.sd_last_error(None) or b"").decode())
 
-    def _here(self, *tensors):
-        if self._device.index != torch.cuda.current_device():
-            _refuse(f"the cache lies on {self._device}, which is not the current device")
+    # (The checks are most of a small call's time on the host, and are written for it: a tensor's attributes take 0.1 us each, torch.Size
+    # objects and t.device more.  A call of append: 10.2 us with a loop over dimensions per tensor, of which the launch is 3.)
+    def _stream_here(self, *tensors):
+        """The current stream, once the current device and the tensors (None: absent) are the cache's."""
+        dev = self._index
         for t in tensors:
-            if t is not None and t.device != self._device:
-                _refuse(f"a tensor lies on {t.device}, the cache on {self._device}")
+            if t is not None and t.get_device() != dev:
+                _refuse(f"a tensor lies on {t.device}, the cache on cuda:{dev}")
+        if torch.cuda.current_device() != dev:
+            _refuse(f"the cache lies on cuda:{dev}, which is not the current device")
+        return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(dev)
 
-    def _indices(self, pos, seq):
-        """Number of rows that pos (and seq) describe, after their checks."""
-        for name, t in (("pos", pos), ("seq", seq)):
-            if t is not None and (t.dtype != torch.int32 or not t.is_contiguous()):
-                _refuse(f"{name} must be a contiguous int32 tensor")
+    def _rows(self, k, v, pos, seq):
+        """(sd_kv_rows of k and v, number of rows), after the checks of what a call that moves rows is given.  k, v: any leading dimensions
+        with one distance between rows, then [n_kv_heads, d_head]."""
         n = pos.numel()
+        if pos.dtype != torch.int32 or not pos.is_contiguous():
+            _refuse("pos must be a contiguous int32 tensor")
         if seq is not None:
-            if seq.numel() != n:
-                _refuse("seq and pos must have an entry per row")
+            if seq.dtype != torch.int32 or not seq.is_contiguous() or seq.numel() != n:
+                _refuse("seq must be a contiguous int32 tensor with an entry per row")
         elif pos.dim() < 2 or pos.shape[0] != self.n_seq:
             _refuse("pos must be [n_seq, rows] where seq is not given")
-        return n
-
-    def _rows(self, k, v, n):
-        """sd_kv_rows of k and v: any leading dimensions with n entries in all and one distance between them, then [n_kv_heads, d_head]."""
-        if k.dtype not in _ROW_TYPES or k.dtype != v.dtype:
+        dtype = _ROW_TYPES.get(k.dtype)
+        if dtype is None or k.dtype != v.dtype:
             _refuse("k and v must be float32 or bfloat16, both the same")
         strides = []
         for t in (k, v):
-            if t.dim() < 3 or t.shape[-2:] != (self.n_kv_heads, self.d_head) or t.numel() != n * self.n_kv_heads * self.d_head:
+            shape = t.shape
+            if len(shape) < 3 or shape[-2] != self.n_kv_heads or shape[-1] != self.d_head or t.numel() != n * self._row_size:
                 _refuse(f"k and v must be [.., {self.n_kv_heads}, {self.d_head}] with a row for each of the {n} positions")
-            strides += _row_strides(t)
-        return _KvRows(k.data_ptr(), v.data_ptr(), *strides, _ROW_TYPES[k.dtype])
+            strides += _row_strides(shape, t.stride()) if n else (0, 0)
+        return _KvRows(k.data_ptr(), v.data_ptr(), *strides, dtype), n
 
     def append(self, k, v, pos, seq=None):
         """sd_kv_append: rows k, v [n_seq, rows, n_kv_heads, d_head] (with seq: [rows, ..]), float32 or bfloat16, to the
         positions pos.  k and v may be views with strides (parts of one projection's output)."""
-        self._here(k, v, pos, seq)
-        n = self._indices(pos, seq)
+        stream = self._stream_here(k, v, pos, seq)
+        rows, n = self._rows(k, v, pos, seq)
         if n:
-            self._check(lib.sd_kv_append(self._ref, C.byref(self._rows(k, v, n)), _ptr(seq), pos.data_ptr(), n, _stream()))
+            self._check(lib.sd_kv_append(self._ref, C.byref(rows), _ptr(seq), pos.data_ptr(), n, stream))
 
     def read(self, pos, seq=None, dtype=torch.bfloat16, k_out=None, v_out=None):
         """sd_kv_read: (k, v) [*pos.shape, n_kv_heads, d_head] at the positions pos; zeros where there is none."""
@@ -254,10 +258,10 @@ class KvCache:
             k_out = torch.empty(*pos.shape, self.n_kv_heads, self.d_head, dtype=dtype, device=self._device)
         if v_out is None:
             v_out = torch.empty(*pos.shape, self.n_kv_heads, self.d_head, dtype=dtype, device=self._device)
-        self._here(k_out, v_out, pos, seq)
-        n = self._indices(pos, seq)
+        stream = self._stream_here(k_out, v_out, pos, seq)
+        rows, n = self._rows(k_out, v_out, pos, seq)
         if n:
-            self._check(lib.sd_kv_read(self._ref, C.byref(self._rows(k_out, v_out, n)), _ptr(seq), pos.data_ptr(), n, _stream()))
+            self._check(lib.sd_kv_read(self._ref, C.byref(rows), _ptr(seq), pos.data_ptr(), n, stream))
         return k_out, v_out
 
     def attention_scratch(self, n_heads: int, rows: int, max_len: int = None) -> torch.Tensor:
@@ -271,18 +275,19 @@ class KvCache:
         """sd_kv_attention: q [n_seq, rows, n_heads, d_head] (float32 or bfloat16) attends to the positions 0 .. pos[n_seq, rows];
         returns out, of q's shape and type.  scale: 1 / sqrt(d_head) by default.  max_len: a bound of the
         contexts, the table's capacity by default.  lse: a float32 tensor [n_seq, rows, n_heads] that receives the logarithms of the sums."""
-        if q.dim() != 4 or q.shape[0] != self.n_seq or q.shape[3] != self.d_head or q.dtype not in _ROW_TYPES:
+        shape, dtype = q.shape, _ROW_TYPES.get(q.dtype)
+        if len(shape) != 4 or shape[0] != self.n_seq or shape[3] != self.d_head or dtype is None:
             _refuse(f"q must be a float32 or bfloat16 tensor [{self.n_seq}, rows, n_heads, {self.d_head}]")
-        S, R, H, D = q.shape
+        S, R, H, D = shape
         if pos.shape != (S, R) or pos.dtype != torch.int32 or not pos.is_contiguous():
             _refuse("pos must be a contiguous int32 tensor [n_seq, rows]")
         if out is None:
             out = torch.empty(S, R, H, D, dtype=q.dtype, device=self._device)
-        elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
+        elif out.shape != shape or out.dtype != q.dtype or not out.is_contiguous():
             _refuse("out must be a contiguous tensor of q's shape and type")
         if lse is not None and (lse.shape != (S, R, H) or lse.dtype != torch.float32 or not lse.is_contiguous()):
             _refuse("lse must be a contiguous float32 tensor [n_seq, rows, n_heads]")
-        if q.numel() == 0:
+        if R == 0 or H == 0:
             return out
         if max_len is None:
             max_len = min(self.capacity, SD_KV_MAX_LEN)
@@ -290,29 +295,31 @@ class KvCache:
             scratch = self.attention_scratch(H, R, max_len)
         elif not scratch.is_contiguous():
             _refuse("scratch must be contiguous")
-        self._here(q, pos, out, lse, scratch)
-        row, head = _row_strides(q)
-        self._check(lib.sd_kv_attention(self._ref, q.data_ptr(), row, head, _ROW_TYPES[q.dtype], pos.data_ptr(), H, R, int(max_len),
+        stream = self._stream_here(q, pos, out, lse, scratch)
+        row, head = _row_strides(shape, q.stride())
+        self._check(lib.sd_kv_attention(self._ref, q.data_ptr(), row, head, dtype, pos.data_ptr(), H, R, int(max_len),
                                         D ** -0.5 if scale is None else float(scale), out.data_ptr(), _ptr(lse), scratch.data_ptr(),
-                                        scratch.numel() * scratch.element_size(), _stream()))
+                                        scratch.nbytes, stream))
         return out
 
 
-def _row_strides(t):
-    """Distances from row to row and from head to head of t [.., heads, d_head]; refuses what has no one distance between rows."""
-    if t.stride(-1) != 1:
+def _row_strides(shape, stride):
+    """Distances from row to row and from head to head of a tensor [.., heads, d_head]; refuses what has no one distance between rows."""
+    if stride[-1] != 1:
         _refuse("the last dimension must be contiguous")
+    if len(shape) == 4 and shape[1] > 1 and shape[2] > 1 and stride[0] == shape[1] * stride[1]:        # (the usual case)
+        return stride[1], stride[2]
     row = None
-    for d in range(t.dim() - 3, -1, -1):                  # leading dimensions, innermost first: each must continue the next
-        if t.shape[d] == 1:
+    for d in range(len(shape) - 3, -1, -1):               # leading dimensions, innermost first: each must continue the next
+        if shape[d] == 1:
             continue
         if row is None:
-            row, reach = t.stride(d), t.stride(d) * t.shape[d]
-        elif t.stride(d) != reach:
+            row, reach = stride[d], stride[d] * shape[d]
+        elif stride[d] != reach:
             _refuse("the rows must lie at one distance")
         else:
-            reach *= t.shape[d]
-    return [row or 0, t.stride(-2) if t.shape[-2] > 1 else 0]
+            reach *= shape[d]
+    return row or 0, stride[-2] if shape[-2] > 1 else 0
 
 
 # --------------------------------------------------------------------------

@@ -37,6 +37,7 @@ sd_status kv_rows(const sd_kv_cache* cache, const sd_kv_rows* x, const int32_t* 
   if (st != SD_OK) return st;
   if (rows < 0) return kv_fail(SD_EINVAL, "negative number of rows");
   if (rows == 0) return SD_OK;
+  if (((int64_t)rows / 8 + 1) * cache->n_kv_heads > 0x7fffffff) return kv_fail(SD_ERANGE, "too many rows");
   if (!x || !x->k || !x->v) return kv_fail(SD_EINVAL, "null rows");
   if (x->dtype != SD_F32 && x->dtype != SD_BF16) return kv_fail(SD_EINVAL, "rows are SD_F32 or SD_BF16");
   if (!aligned16(x->k) || !aligned16(x->v)) return kv_fail(SD_EINVAL, "rows must be 16-byte aligned");
@@ -53,16 +54,16 @@ sd_status kv_rows(const sd_kv_cache* cache, const sd_kv_rows* x, const int32_t* 
 }
 
 // The checks that the scratch's size depends on.
-sd_status kv_attention_plan(const sd_kv_cache* c, int32_t n_heads, int32_t rows, int32_t max_len, sd::KvPlan& p) {
+sd_status kv_attention_plan(const sd_kv_cache* c, int32_t n_heads, int32_t rows, int32_t max_len, int32_t dtype, sd::KvPlan& p) {
   if (n_heads < 1 || n_heads % c->n_kv_heads) return kv_fail(SD_EINVAL, "n_heads must be a multiple of n_kv_heads");
   if (rows < 1) return kv_fail(SD_EINVAL, "rows must be positive");
   if (max_len < 1 || max_len > SD_KV_MAX_LEN) return kv_fail(SD_ERANGE, "max_len outside 1 .. SD_KV_MAX_LEN");
   if (c->n_seq > 65535) return kv_fail(SD_ERANGE, "more than 65535 sequences");
   const int64_t pairs = (int64_t)rows * (n_heads / c->n_kv_heads);
   if (pairs > 65535 || (int64_t)c->n_seq * rows * n_heads > 0x7fffffff / 128) return kv_fail(SD_ERANGE, "too many rows");
-  p = sd::kv_plan(c->n_seq, c->n_kv_heads, (int)pairs, max_len);
+  p = sd::kv_plan(c->n_seq, c->n_kv_heads, (int)pairs, max_len, c->d_head, c->dtype == SD_E4M3, dtype == SD_F32);
   if ((int64_t)c->n_seq * c->n_kv_heads * p.groups > SD_KV_MAX_GROUPS || (int64_t)p.groups * p.n_ranges > 65535)
-    return kv_fail(SD_ERANGE, "more than SD_KV_MAX_GROUPS (sequence, 32 rows, kv head)s");
+    return kv_fail(SD_ERANGE, "more than SD_KV_MAX_GROUPS (sequence, 16 rows, kv head)s");
   return SD_OK;
 }
 }  // namespace
@@ -77,9 +78,14 @@ extern "C" sd_status sd_kv_read(const sd_kv_cache* cache, const sd_kv_rows* rows
 
 extern "C" size_t sd_kv_attention_scratch_bytes(const sd_kv_cache* cache, int32_t n_heads, int32_t rows, int32_t max_len) {
   sd::KvCacheArgs a{};
-  sd::KvPlan p{};
-  if (kv_cache_args(cache, a) != SD_OK || kv_attention_plan(cache, n_heads, rows, max_len, p) != SD_OK) return 0;
-  return sd::kv_scratch_bytes(cache->n_seq, cache->n_kv_heads, cache->d_head, p);
+  size_t most = 0;
+  for (int32_t dtype : {SD_F32, SD_BF16}) {          // (they are cut differently)
+    sd::KvPlan p{};
+    if (kv_cache_args(cache, a) != SD_OK || kv_attention_plan(cache, n_heads, rows, max_len, dtype, p) != SD_OK) return 0;
+    const size_t n = sd::kv_scratch_bytes(cache->n_seq, cache->n_kv_heads, cache->d_head, p);
+    if (n > most) most = n;
+  }
+  return most;
 }
 
 extern "C" sd_status sd_kv_attention(const sd_kv_cache* cache, const void* q, int64_t q_row_stride, int64_t q_head_stride, int32_t dtype, const int32_t* pos,
@@ -88,10 +94,10 @@ extern "C" sd_status sd_kv_attention(const sd_kv_cache* cache, const void* q, in
   sd::KvAttnArgs a{};
   sd::KvPlan p{};
   sd_status st = kv_cache_args(cache, a.c);
-  if (st == SD_OK) st = kv_attention_plan(cache, n_heads, rows, max_len, p);
+  if (st == SD_OK && dtype != SD_F32 && dtype != SD_BF16) st = kv_fail(SD_EINVAL, "queries are SD_F32 or SD_BF16");
+  if (st == SD_OK) st = kv_attention_plan(cache, n_heads, rows, max_len, dtype, p);
   if (st != SD_OK) return st;
   if (!q || !pos || !out || !scratch) return kv_fail(SD_EINVAL, "null pointer");
-  if (dtype != SD_F32 && dtype != SD_BF16) return kv_fail(SD_EINVAL, "queries are SD_F32 or SD_BF16");
   if (!aligned16(q) || !aligned16(out) || !aligned16(scratch)) return kv_fail(SD_EINVAL, "q, out and scratch must be 16-byte aligned");
   if ((q_row_stride | q_head_stride) & 7) return kv_fail(SD_EINVAL, "strides must be multiples of 8 elements");
   if (!(scale > 0.0f) || !std::isfinite(scale)) return kv_fail(SD_EINVAL, "scale must be positive");
@@ -99,11 +105,12 @@ extern "C" sd_status sd_kv_attention(const sd_kv_cache* cache, const void* q, in
   a.q = q; a.q_row = q_row_stride; a.q_head = q_head_stride; a.out = out; a.lse = lse; a.pos = pos;
   a.R = rows; a.H = n_heads; a.G = n_heads / cache->n_kv_heads;
   a.groups = p.groups; a.rows_wg = p.rows_wg; a.max_len = max_len; a.range_keys = p.range_keys; a.n_ranges = p.n_ranges;
+  a.n_seq = cache->n_seq; a.by_g.set(a.G); a.by_groups.set(a.groups); a.by_hkv.set(a.c.Hkv);
   a.c_log2 = scale * 1.44269504088896340736f;
   a.tickets = static_cast<unsigned*>(scratch);
   a.partial = reinterpret_cast<float*>(static_cast<char*>(scratch) + sd::KV_TICKET_BYTES);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (dtype == SD_F32) sd::launch_kv_attention<float>(s, a, cache->d_head, cache->dtype == SD_E4M3, cache->n_seq);
-  else sd::launch_kv_attention<sd::bf16>(s, a, cache->d_head, cache->dtype == SD_E4M3, cache->n_seq);
+  if (dtype == SD_F32) sd::launch_kv_attention<float>(s, a, cache->d_head, cache->dtype == SD_E4M3, cache->n_seq, p);
+  else sd::launch_kv_attention<sd::bf16>(s, a, cache->d_head, cache->dtype == SD_E4M3, cache->n_seq, p);
   return hipGetLastError() == hipSuccess ? SD_OK : kv_fail(SD_EHIP, "kernel launch");
 }

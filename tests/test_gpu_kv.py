@@ -231,7 +231,7 @@ def test_no_rows_and_rows_without_a_position_list():
     assert torch.equal(cache.pool, before)
     # the C entry without positions: 0, 1, .. of each sequence
     x = normal(g, 2, 5, 2, 64)
-    rows = cache._rows(x, x, 10)
+    rows = binding._KvRows(x.data_ptr(), x.data_ptr(), 128, 64, 128, 64, binding.SD_BF16)
     assert binding.lib.sd_kv_append(cache._ref, rows, None, None, 10, binding._stream()) == binding.SD_OK
     k, _ = cache.read(torch.arange(5, dtype=torch.int32, device="cuda").repeat(2, 1).contiguous())
     c, e = quantised(x)
@@ -276,6 +276,40 @@ def test_attention_over_every_number_of_rows(dtype, cache_dtype, H, Hkv, R):
 
 
 @pytest.mark.parametrize("cache_dtype", ["e4m3", "bf16"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("S,H,Hkv,R", [(2, 32, 8, 1), (2, 32, 8, 5), (2, 32, 8, 9), (8, 8, 8, 16), (8, 16, 8, 17)])
+def test_attention_cut_for_long_contexts(dtype, cache_dtype, S, H, Hkv, R):
+    """Calls that are cut for contexts of 40000, whatever theirs are: one and two tiles, one and several groups; table entries behind a context are anything."""
+    D, max_len = 128, 40000
+    lens = [700, 33, 5, 1000, 1, 64, 257, 500][:S]
+    cache, g = make(S, 64, Hkv, D, 16, cache_dtype, 20)
+    wide = torch.randint(-5, cache.pool.shape[0] + 5, (S, 2500), dtype=torch.int32, device="cuda", generator=g)
+    wide[:, :64] = cache.page_table
+    plain = fill(cache, g, lens, dtype=dtype)
+    cache = type(cache)(wide, cache.pool.shape[0], Hkv, D, dtype=cache_dtype, pool=cache.pool, exps=cache.exps)
+    q = normal(g, S, R, H, D, dtype=dtype, std=2.0)
+    pos = torch.tensor([[L - R + r for r in range(R)] for L in lens], dtype=torch.int32, device="cuda")
+    pos[1, 0] = 32
+    lse = torch.empty(S, R, H, device="cuda")
+    out = cache.attention(q, pos, max_len=max_len, lse=lse)
+    check_attention(out, lse, q, plain, pos)
+    assert torch.equal(out, cache.attention(q, pos, max_len=max_len))
+
+
+@pytest.mark.parametrize("cache_dtype", ["e4m3", "bf16"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,Hkv,D,R,max_len", [(32, 8, 128, 1, 700), (32, 8, 128, 5, 2600), (64, 32, 64, 1, 1200), (16, 16, 32, 3, 3000)])
+def test_attention_with_eight_wavefronts(dtype, cache_dtype, H, Hkv, D, R, max_len):
+    lens = [700, 512, 257, 256, 255, 1, 33, 600]
+    cache, g = make(8, -(-max_len // 16), Hkv, D, 16, cache_dtype, 21)
+    plain = fill(cache, g, lens, dtype=dtype)
+    q = normal(g, 8, R, H, D, dtype=dtype, std=2.0)
+    pos = torch.tensor([[L - R + r for r in range(R)] for L in lens], dtype=torch.int32, device="cuda")
+    lse = torch.empty(8, R, H, device="cuda")
+    check_attention(cache.attention(q, pos, max_len=max_len, lse=lse), lse, q, plain, pos)
+
+
+@pytest.mark.parametrize("cache_dtype", ["e4m3", "bf16"])
 @pytest.mark.parametrize("n", [66000, 131072])
 def test_attention_over_a_very_long_context(cache_dtype, n):
     cache, g = make(1, n // 64 + 1, 2, 64, 64, cache_dtype, 8)
@@ -302,13 +336,17 @@ def test_attention_with_flat_and_peaked_weights(scale, dtype):
 
 
 @pytest.mark.parametrize("cache_dtype", ["e4m3", "bf16"])
-@pytest.mark.parametrize("R", [4, 20])
+@pytest.mark.parametrize("R,max_len", [(4, None), (20, None), (12, 140000), (20, 140000)])
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
-def test_rows_are_not_reached_by_what_they_do_not_see(cache_dtype, R, bad):
+def test_rows_are_not_reached_by_what_they_do_not_see(cache_dtype, R, max_len, bad):
     """K and V of the last rows are not finite: rows before them are as if they were, rows that see them are not finite either."""
     n = 600
     cache, g = make(2, 48, 2, 128, 16, cache_dtype, 10)
     plain = fill(cache, g, [n, n])
+    if max_len is not None:                            # (two tiles of rows)
+        table = torch.zeros(2, max_len // 16, dtype=torch.int32, device="cuda")
+        table[:, :48] = cache.page_table
+        cache = type(cache)(table, cache.pool.shape[0], 2, 128, dtype=cache_dtype, pool=cache.pool, exps=cache.exps)
     q = normal(g, 2, R, 4, 128)
     pos = torch.tensor([[n - R + r for r in range(R)]] * 2, dtype=torch.int32, device="cuda")
     pos[1, 1] = -1

@@ -56,6 +56,7 @@ def test_bad_rows_are_refused(kw, word):
 def test_bad_numbers_of_rows_are_refused_and_none_is_fine():
     for f in (b.lib.sd_kv_append, b.lib.sd_kv_read):
         refused(b.SD_EINVAL, "negative", f(C.byref(cache()), C.byref(rows()), None, AT, -1, None))
+        refused(b.SD_ERANGE, "too many", f(C.byref(cache(n_kv_heads=64)), C.byref(rows()), None, AT, 0x7ffffffc, None))
         refused(b.SD_EINVAL, "same number", f(C.byref(cache()), C.byref(rows()), None, AT, 5, None))
         refused(b.SD_EINVAL, "null", f(C.byref(cache()), None, None, AT, 4, None))
         refused(b.SD_EINVAL, "null", f(None, C.byref(rows()), None, AT, 4, None))
