@@ -62,10 +62,18 @@ enum {
                            front instead of in order.  Results are identical; it exists to show that
                            every kernel finds its pages through the table.  sd_set_flags leaves it as
                            it was at load. */
-  SD_FLAG_SEPARATE_CROSS_Q = 16 /* small T5-type models (bf16, heads of 64, d_model <= 512, at most 16 rows)
+  SD_FLAG_SEPARATE_CROSS_Q = 16, /* small T5-type models (bf16, heads of 64, d_model <= 512, at most 16 rows)
                            let the cross-attention kernel compute its own queries, one launch less
                            per layer; with this flag the query projection stays a launch of its own.
                            Results are identical; it exists so that a test can show that. */
+  SD_FLAG_KV_E4M3 = 32  /* at load only: the target keeps its KV cache in 8 bits (SD_E4M3 of sd_kv_cache below: a power of
+                           two per position, head and K or V), half the memory of bf16 and a quarter of
+                           fp32, and attends over it as sd_kv_attention does; a prompt's passes read it back.  A
+                           workspace also holds one layer's cache in the model's dtype.  Mq's cache stays
+                           as it is.  Not for T5DEC targets (SD_EINVAL).  Results differ by the rounding of keys and
+                           values (2^-4 relative); a row's do not depend on gamma or on the
+                           other rows, but on the number of sequences the context was loaded for, by
+                           the order of sums.  sd_set_flags leaves it as it was at load. */
 };
 
 /*
@@ -247,7 +255,7 @@ const char* sd_last_error(const sd_ctx* ctx);
 sd_status sd_debug_logits(sd_ctx* ctx, int32_t which, float* host_out, size_t n);
 sd_status sd_get_stats(sd_ctx* ctx, sd_stats* out);
 /* Replace the flags given at load for the following calls (captured graphs are rebuilt).
- * SD_FLAG_SCATTER_PAGES keeps the value it had at load whatever is passed here. */
+ * SD_FLAG_SCATTER_PAGES and SD_FLAG_KV_E4M3 keep the values they had at load whatever is passed here. */
 sd_status sd_set_flags(sd_ctx* ctx, int32_t flags);
 /* Sampling options for the following sd_step / sd_step_baseline calls (host
  * struct, copied).  SD_EINVAL unless 0 < lenience <= 1, top_k >= 0,

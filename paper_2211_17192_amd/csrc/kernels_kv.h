@@ -302,6 +302,7 @@ struct KvAttnArgs {
 // slots behind the last key may be read, and whatever lies there (NaN too) is replaced by zeros before the product.
 // Rows that see fewer keys than others of the same workgroup: where V of a key that some row does not see is not finite, zeros enter the product
 // and a product of ones marks the rows that see it (0 * NaN would reach the others).
+// Every sum is spelled out (fmaf), so that all builds of this kernel give a row the same bits.
 // grid = (pairs of sequence and kv head x groups, ranges).  Workgroups take turns on the XCDs, so the groups of a pair, which read the same keys and
 // values at about the same time, lie eight apart: one of them comes from memory, the others find the lines in their L2.
 template <typename T, int DH, int NW, int NRT, bool E4M3> struct KvShape {
@@ -632,7 +633,7 @@ static __global__ __launch_bounds__(64 * NW, 2) void kv_attention_kernel(const K
           sc[kt][rt][r] = __builtin_amdgcn_exp2f(fmaf(sc[kt][rt][r], a.c_log2, -ref));
           sum += sc[kt][rt][r];
         }
-      l_run[rt] = l_run[rt] * f[rt] + sum;           // this lane's keys; the quarters are added at the end
+      l_run[rt] = fmaf(l_run[rt], f[rt], sum);       // this lane's keys; the quarters are added at the end
       m_run[rt] = m_new;
     }
     if (__builtin_amdgcn_ballot_w64(rescale) != 0ull) {
@@ -685,7 +686,7 @@ static __global__ __launch_bounds__(64 * NW, 2) void kv_attention_kernel(const K
   auto write = [&](int g, int d, const f32x4& x, float m, float l) {           // the finished features d .. d + 3 of pair g
     const int r = a.by_g.quotient(rg0 + g), h = hkv * G + rg0 + g - r * G, row = seq * a.R + r;
     const bool none = l == 0.0f;
-    if (a.lse != nullptr && d == 0) a.lse[(size_t)row * a.H + h] = none ? -INFINITY : m * 0.6931471805599453f + logf(l);
+    if (a.lse != nullptr && d == 0) a.lse[(size_t)row * a.H + h] = none ? -INFINITY : fmaf(m, 0.6931471805599453f, logf(l));
     f32x4 y;
 #pragma unroll
     for (int e = 0; e < 4; ++e) y[e] = none ? 0.0f : x[e] / l;
@@ -725,9 +726,9 @@ static __global__ __launch_bounds__(64 * NW, 2) void kv_attention_kernel(const K
 #pragma unroll
       for (int w = 0; w < NW; ++w) {                 // (a wavefront without keys, and a row without any, count as nothing)
         const float e = (mw[w] == -INFINITY) ? 0.0f : __builtin_amdgcn_exp2f(mw[w] - m);
-        L += lw[w] * e;
+        L = fmaf(lw[w], e, L);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) acc[r] += (mw[w] == -INFINITY && lw[w] == 0.0f) ? 0.0f : ow[w][r] * e;
+        for (int r = 0; r < 4; ++r) acc[r] = (mw[w] == -INFINITY && lw[w] == 0.0f) ? acc[r] : fmaf(ow[w][r], e, acc[r]);
       }
       const int rg = rt * KV_ROWS + g;
       if (n_act == 1) write(rg, d, acc, m, L);
@@ -775,7 +776,7 @@ static __global__ __launch_bounds__(64 * NW, 2) void kv_attention_kernel(const K
     for (int x = j; x < n_act; x += 16) {
       const float2 p = ml[x * RG + g];
       const float e = (p.x == -INFINITY) ? 0.0f : __builtin_amdgcn_exp2f(p.x - m);
-      L += p.y * e;
+      L = fmaf(p.y, e, L);
       ml[x * RG + g].x = e;
     }
     L = lane_combine<1>(L, OpSumF()); L = lane_combine<2>(L, OpSumF()); L = lane_combine<4>(L, OpSumF()); L = lane_combine<8>(L, OpSumF());
@@ -793,7 +794,7 @@ static __global__ __launch_bounds__(64 * NW, 2) void kv_attention_kernel(const K
         for (int u = 0; u < NB; ++u)
           if (x0 + u * parts < n_act) {
             const float w = ml[(x0 + u * parts) * RG + g].x;
-            acc[0] += lo[u].x * w; acc[1] += lo[u].y * w; acc[2] += hi[u].x * w; acc[3] += hi[u].y * w;
+            acc[0] = fmaf(lo[u].x, w, acc[0]); acc[1] = fmaf(lo[u].y, w, acc[1]); acc[2] = fmaf(hi[u].x, w, acc[2]); acc[3] = fmaf(hi[u].y, w, acc[3]);
           }
       }
     }
@@ -826,30 +827,39 @@ constexpr size_t KV_TICKET_BYTES = (size_t)KV_TICKETS * sizeof(unsigned);
 //   in one range (15.3, 16.8 in two); nor more than the join is worth (one of 8192 in 8, 16, 32 ranges 13.9, 11.7, 13.3; of 32768 in 16, 32, 64 20.9, 19.0, 23.9).
 //   At most 4096 keys (64 of 8192 in ranges of 1024, 2048, 4096 207, 192, 181; contexts between a quarter of that and all of it 143, 140, 144).
 //   Eight wavefronts where a CU has one workgroup of 512 keys or more (16 of 2048 15.3, 17.3 with four; 64 of 2048 53.9, 52.3), unless they are few (one of 1000 9.7, 8.4).
-struct KvPlan { int rows_wg, groups, range_keys, n_ranges, waves; bool once; };
-inline KvPlan kv_plan(int n_seq, int Hkv, int pairs, int max_len, int d_head, bool e4m3, bool f32) {
-  KvPlan p;
-  const long long heads = (long long)n_seq * Hkv;
-  const bool large = heads * max_len * 2 * d_head * (e4m3 ? 1 : 2) >= 128ll << 20;
-  const int most = (large && !f32) ? 2 * KV_ROWS : KV_ROWS;
-  p.groups = (pairs + most - 1) / most;
-  p.rows_wg = (pairs + p.groups - 1) / p.groups;
-  p.once = large && p.groups == 1;
-  const long long wgs = heads * p.groups, per_cu = wgs < 256 ? 256 / wgs : 1;
+struct KvPlan { int rows_wg, groups, range_keys, n_ranges, waves; bool large, once; };
+// What the sums of a row depend on: the ranges and the wavefronts.  wgs: (sequence, kv head, group)s.
+inline void kv_plan_ranges(KvPlan& p, long long wgs, long long heads, int max_len, int d_head, bool e4m3) {
+  p.large = heads * max_len * 2 * d_head * (e4m3 ? 1 : 2) >= 128ll << 20;
+  const long long per_cu = wgs < 256 ? 256 / wgs : 1;
   const long long work = (long long)max_len * d_head / 128;                    // keys, by what a step over them takes
   long long ranges = 1;
-  if (large) ranges = per_cu;
+  if (p.large) ranges = per_cu;
   else if (work >= (per_cu > 2 ? 768 : 2560)) {
     ranges = per_cu < (work + 255) / 256 ? per_cu : (work + 255) / 256;
     while (ranges > 1 && 100 * ranges * ranges > 3 * work) --ranges;
   }
   long long keys = (max_len + ranges - 1) / ranges;
-  p.waves = (!large && wgs >= 64 && wgs <= 256 && keys * d_head / 128 >= 512) ? 8 : 4;
+  p.waves = (!p.large && wgs >= 64 && wgs <= 256 && keys * d_head / 128 >= 512) ? 8 : 4;
   const long long unit = 32 * p.waves, least = ((long long)max_len + KV_MAX_RANGES - 1) / KV_MAX_RANGES, longest = KV_MAX_RANGE_KEYS;
   if (keys > longest) keys = longest;
   if (keys < least) keys = least;
   p.range_keys = (int)((keys + unit - 1) / unit * unit);
   p.n_ranges = (max_len + p.range_keys - 1) / p.range_keys;
+}
+// What they do not depend on: how the rows are grouped.
+inline void kv_plan_rows(KvPlan& p, long long heads, int pairs, int max_len, int d_head, bool e4m3, bool f32) {
+  p.large = heads * max_len * 2 * d_head * (e4m3 ? 1 : 2) >= 128ll << 20;
+  const int most = (p.large && !f32) ? 2 * KV_ROWS : KV_ROWS;
+  p.groups = (pairs + most - 1) / most;
+  p.rows_wg = (pairs + p.groups - 1) / p.groups;
+  p.once = p.large && p.groups == 1;
+}
+inline KvPlan kv_plan(int n_seq, int Hkv, int pairs, int max_len, int d_head, bool e4m3, bool f32) {
+  KvPlan p{};
+  const long long heads = (long long)n_seq * Hkv;
+  kv_plan_rows(p, heads, pairs, max_len, d_head, e4m3, f32);
+  kv_plan_ranges(p, heads * p.groups, heads, max_len, d_head, e4m3);
   return p;
 }
 inline size_t kv_scratch_bytes(int n_seq, int Hkv, int d_head, const KvPlan& p) {
@@ -879,7 +889,10 @@ template <typename T> void launch_kv_rows(hipStream_t s, const KvRowsArgs& a, in
     else launch(std::false_type());
   });
 }
-// a.groups, rows_wg, range_keys and n_ranges: the plan's.
+inline void kv_set_plan(KvAttnArgs& a, const KvPlan& p) {          // (a.G, a.c and a.n_seq are set)
+  a.groups = p.groups; a.rows_wg = p.rows_wg; a.range_keys = p.range_keys; a.n_ranges = p.n_ranges;
+  a.by_g.set(a.G); a.by_groups.set(a.groups); a.by_hkv.set(a.c.Hkv);
+}
 template <typename T> void launch_kv_attention(hipStream_t s, const KvAttnArgs& a, int d_head, bool e4m3, int n_seq, const KvPlan& p) {
   kv_with_head(d_head, [&](auto dh) {
     constexpr int DH = decltype(dh)::value;

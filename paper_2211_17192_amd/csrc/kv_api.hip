@@ -104,8 +104,8 @@ extern "C" sd_status sd_kv_attention(const sd_kv_cache* cache, const void* q, in
   if (scratch_bytes < sd::kv_scratch_bytes(cache->n_seq, cache->n_kv_heads, cache->d_head, p)) return kv_fail(SD_ENOMEM, "scratch too small: see sd_kv_attention_scratch_bytes");
   a.q = q; a.q_row = q_row_stride; a.q_head = q_head_stride; a.out = out; a.lse = lse; a.pos = pos;
   a.R = rows; a.H = n_heads; a.G = n_heads / cache->n_kv_heads;
-  a.groups = p.groups; a.rows_wg = p.rows_wg; a.max_len = max_len; a.range_keys = p.range_keys; a.n_ranges = p.n_ranges;
-  a.n_seq = cache->n_seq; a.by_g.set(a.G); a.by_groups.set(a.groups); a.by_hkv.set(a.c.Hkv);
+  a.n_seq = cache->n_seq; a.max_len = max_len;
+  sd::kv_set_plan(a, p);
   a.c_log2 = scale * 1.44269504088896340736f;
   a.tickets = static_cast<unsigned*>(scratch);
   a.partial = reinterpret_cast<float*>(static_cast<char*>(scratch) + sd::KV_TICKET_BYTES);

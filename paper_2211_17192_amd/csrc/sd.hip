@@ -52,6 +52,7 @@ struct LayerW {
   void *lncg = nullptr, *cq = nullptr, *ck = nullptr, *cv = nullptr, *co = nullptr;
   void *ln2g = nullptr, *ln2b = nullptr, *w1 = nullptr, *wu = nullptr, *b1 = nullptr, *w2 = nullptr, *b2 = nullptr;
   void* kv = nullptr;                       // [page][2][Hkv][PS][dh]
+  unsigned char* kv_exps = nullptr;         // kv in e4m3: [page][2][Hkv][PS]
   void *cross_k = nullptr, *cross_v = nullptr;   // [H][enc_len][dh]
 };
 
@@ -79,6 +80,13 @@ struct Model {
   void* xfrag2 = nullptr;          // a batched kernel's output that the next product reads, in fragment order
   int attn_nsplit = 1, attn_split_keys = 0;   // long contexts: key ranges per (sequence, kv head)
   float* attn_partial = nullptr;
+  // SD_FLAG_KV_E4M3: the layers' caches in 8 bits.  A pass writes its keys and values in the storage type into kv_stage, which has the
+  // geometry of one layer's cache, and from there to the layer's
+  bool kv_e4m3 = false;
+  void* kv_stage = nullptr;
+  KvPlan kv_plan{};            // how its attention is cut; the grouping of the rows is each call's
+  unsigned* kv_tickets = nullptr;
+  float* kv_partial = nullptr;
   float* x = nullptr;
   void* xg = nullptr;          // x * gain of the next RMSNorm, storage type
   float* ss = nullptr;         // [d_model/16][16] partial sums of x^2
@@ -122,9 +130,12 @@ int prompt_rows_per_wg(const sd_model_cfg& c) { return ATTN_MAX_RG / (c.n_heads 
 // results.  Below 32 rows there are no such passes (forward()'s kernels take 16 rows at a time).
 constexpr int ROWS_PASS_MAX = 2048, ROWS_PASS_MIN = 32;
 
+constexpr int KV_MODEL_GROUPS = ATTN_MAX_RG / KV_ROWS;   // of (row, query head) pairs of a kv head
+
 // Lays a model out in the arena (or sizes it); rows_limit: prompt rows of one pass at most, 0: no such passes.
-void plan_model(Arena& A, Model& m, const sd_model_cfg& c, int page_size, int batch, int rows_limit) {
+void plan_model(Arena& A, Model& m, const sd_model_cfg& c, int page_size, int batch, int rows_limit, bool kv_e4m3) {
   m.cfg = c;
+  m.kv_e4m3 = kv_e4m3;
   m.batch = batch;
   // bf16 models with the matrix-core attention take a prompt many rows at a time
   const bool many = rows_limit > 0 && c.dtype == SD_BF16 && (c.d_head == 64 || c.d_head == 128);
@@ -168,7 +179,17 @@ void plan_model(Arena& A, Model& m, const sd_model_cfg& c, int page_size, int ba
       l.cross_k = A.take((size_t)c.enc_len * m.nq * e);
       l.cross_v = A.take((size_t)c.enc_len * m.nq * e);
     }
-    l.kv = A.take((size_t)batch * m.n_pages * 2 * c.n_kv_heads * page_size * c.d_head * e);
+    const size_t kv_rows = (size_t)batch * m.n_pages * 2 * c.n_kv_heads * page_size;
+    l.kv = A.take(kv_rows * c.d_head * (kv_e4m3 ? 1 : e));
+    if (kv_e4m3) l.kv_exps = static_cast<unsigned char*>(A.take(kv_rows));
+  }
+  if (kv_e4m3) {
+    m.kv_stage = A.take((size_t)batch * m.n_pages * 2 * c.n_kv_heads * page_size * c.d_head * e);
+    // (whatever the number of rows, so that a row's sums never depend on it)
+    const long long heads = (long long)batch * c.n_kv_heads;
+    kv_plan_ranges(m.kv_plan, heads, heads, c.max_len, c.d_head, true);
+    m.kv_tickets = static_cast<unsigned*>(A.take((size_t)heads * KV_MODEL_GROUPS * sizeof(unsigned)));
+    m.kv_partial = static_cast<float*>(A.take(m.kv_plan.n_ranges > 1 ? (size_t)heads * m.kv_plan.n_ranges * ATTN_MAX_RG * (c.d_head + 2) * sizeof(float) : 0));
   }
   const size_t rows = (size_t)m.rows_cap;
   m.page_table = static_cast<int*>(A.take((size_t)batch * m.n_pages * sizeof(int)));
@@ -266,8 +287,8 @@ namespace {
 void plan_ctx(Arena& A, sd_ctx& c, const sd_model_cfg& pc, const sd_model_cfg& qc, const sd_runtime_cfg& rt, int rows_limit) {
   const size_t B = (size_t)rt.batch;
   c.batch = rt.batch;
-  plan_model(A, c.p, pc, rt.page_size, rt.batch, rows_limit);
-  plan_model(A, c.q, qc, rt.page_size, rt.batch, rows_limit);
+  plan_model(A, c.p, pc, rt.page_size, rt.batch, rows_limit, (rt.flags & SD_FLAG_KV_E4M3) != 0);
+  plan_model(A, c.q, qc, rt.page_size, rt.batch, rows_limit, false);
   c.d_state = static_cast<SeqState*>(A.take(B * sizeof(SeqState)));
   c.d_params = static_cast<StepParams*>(A.take(B * sizeof(StepParams)));
   c.p_logits = static_cast<float*>(A.take(B * (rt.max_gamma + 1) * pc.vocab * sizeof(float)));   // [seq][gamma+1][V]
@@ -291,6 +312,15 @@ bool rt_ok(const sd_runtime_cfg& rt, std::string& why) {
   if (rt.batch < 1 || rt.batch > SD_MAX_BATCH) { why = "batch out of range"; return false; }
   if (rt.max_gamma < 1 || rt.max_gamma > SD_MAX_GAMMA) { why = "max_gamma out of range"; return false; }
   if (rt.page_size < 16 || (rt.page_size & (rt.page_size - 1))) { why = "page_size must be a power of two >= 16"; return false; }
+  return true;
+}
+
+// Whether the target may have its cache in 8 bits.
+bool kv_flag_ok(const sd_model_cfg& pc, const sd_runtime_cfg& rt, std::string& why) {
+  if (!(rt.flags & SD_FLAG_KV_E4M3)) return true;
+  if (pc.arch == SD_ARCH_T5DEC) { why = "SD_FLAG_KV_E4M3: the attention over 8-bit caches has no position bias (T5DEC targets)"; return false; }
+  if (pc.max_len > SD_KV_MAX_LEN) { why = "SD_FLAG_KV_E4M3: max_len beyond SD_KV_MAX_LEN"; return false; }
+  if ((int64_t)rt.batch * pc.n_kv_heads * KV_MODEL_GROUPS > SD_KV_MAX_GROUPS) { why = "SD_FLAG_KV_E4M3: too many kv heads"; return false; }
   return true;
 }
 
@@ -705,6 +735,42 @@ void launch_embed_any(sd_ctx* c, Model& m, const Rows& rw) {
   else launch_embed<float>(c, m, rw);
 }
 
+// ---- the target's cache in 8 bits (kernels_kv.h) ----
+KvRowsArgs kv_rows_args(const Model& m, const LayerW& l, int rows) {
+  KvRowsArgs a{};
+  a.c.pool = l.kv; a.c.exps = l.kv_exps; a.c.table = m.page_table; a.c.n_pages = m.batch * m.n_pages; a.c.n_seq = m.batch; a.c.table_stride = m.n_pages;
+  a.c.page_shift = __builtin_ctz((unsigned)m.page_size); a.c.Hkv = m.cfg.n_kv_heads;
+  a.rows = rows; a.per_seq = rows; a.k = a.v = m.kv_stage; a.paged = 1;
+  return a;
+}
+// The keys and values that a pass over `rows` rows has left in kv_stage, into the layer's cache.  (The product's epilogue cannot: a head's largest magnitude
+// is spread over the workgroups that hold its 16-feature tiles.)
+template <typename T> void kv_append_stage(const Model& m, const LayerW& l, int rows) {
+  KvRowsArgs a = kv_rows_args(m, l, rows);
+  a.seq = m.row_seq; a.pos = m.row_pos;
+  launch_kv_rows<T>(m.stream, a, m.cfg.d_head, true, true);
+}
+// A prompt's attention is that of the storage type over kv_stage, with the cache's own values there: positions 0 .. n - 1 of sequence seq.
+template <typename T> void kv_read_stage(const Model& m, const LayerW& l, int seq, int n) {
+  KvRowsArgs a = kv_rows_args(m, l, n);
+  a.c.table += (size_t)seq * m.n_pages; a.c.n_seq = 1;
+  launch_kv_rows<T>(m.stream, a, m.cfg.d_head, true, false);
+}
+template <typename T> void kv_attention(const Model& m, const LayerW& l, const Rows& rw, bf16* out_frag) {
+  const sd_model_cfg& f = m.cfg;
+  KvAttnArgs a{};
+  a.c = kv_rows_args(m, l, 0).c;
+  a.R = rw.rps; a.H = f.n_heads; a.G = f.n_heads / f.n_kv_heads; a.seq0 = rw.seq0; a.n_seq = rw.nseq;
+  a.q = m.qbuf; a.q_row = m.nq; a.q_head = f.d_head; a.out = m.attn; a.pos = m.row_pos; a.max_len = f.max_len;
+  if (out_frag != nullptr) { a.out_frag = out_frag; a.frag_ks = 1; a.frag_slab = m.nq / 32; }
+  KvPlan p = m.kv_plan;
+  kv_plan_rows(p, (long long)m.batch * f.n_kv_heads, a.R * a.G, f.max_len, f.d_head, true, sizeof(T) == 4);
+  kv_set_plan(a, p);
+  a.c_log2 = 1.44269504088896340736f / sqrtf((float)f.d_head);
+  a.tickets = m.kv_tickets; a.partial = m.kv_partial;
+  launch_kv_attention<T>(m.stream, a, f.d_head, true, rw.nseq, p);
+}
+
 // One forward of model m; with `logits` the LM head runs on every row and each row's
 // output goes where the embedding kernel's row map says (or nowhere); without (a prompt) the last layer ends at
 // its cache append.
@@ -807,11 +873,12 @@ void forward(sd_ctx* c, Model& m, const Rows& rw, float* logits) {
       const size_t nq0 = cache_only ? m.nq : 0;      // features left out: the queries
       a.W = static_cast<const char*>(l.wqkv) + nq0 * d * e; a.K = d; a.N = m.nq + 2 * m.nkv - (int)nq0;
       a.bias = l.bqkv ? static_cast<const char*>(l.bqkv) + nq0 * e : nullptr;
-      a.q_out = q.qbuf; a.nq = m.nq - (int)nq0; a.nkv = m.nkv; a.kv_pool = l.kv; a.page_table = m.page_table;
+      a.q_out = q.qbuf; a.nq = m.nq - (int)nq0; a.nkv = m.nkv; a.kv_pool = m.kv_e4m3 ? m.kv_stage : l.kv; a.page_table = m.page_table;
       a.page_size = m.page_size; a.n_kv_heads = f.n_kv_heads; a.d_head = f.d_head; a.row_pos = q.row_pos;
       a.rope = m.rope;
       if (m.batch > 1) { a.row_seq = q.row_seq; a.pt_stride = m.n_pages; }
     });
+    if (m.kv_e4m3 && !(skip & SD_OP_QKV)) kv_append_stage<T>(m, l, rows_total);
     if (cache_only) break;
     // Small models: the cross-attention kernel computes its own queries (ATTN_CROSS_PROJ), one launch
     // less per layer.  The conditions are the kernel's: bf16, heads of 64, one query head per kv head,
@@ -821,10 +888,12 @@ void forward(sd_ctx* c, Model& m, const Rows& rw, float* logits) {
                               f.n_heads == f.n_kv_heads && n_groups == 1 && d <= 512 && d % 32 == 0 &&
                               !(c->rt.flags & SD_FLAG_SEPARATE_CROSS_Q);
     auto attention = [&](bool cross) {
+      if (m.kv_e4m3 && rw.mode != ROWS_PREFILL) { kv_attention<T>(m, l, rw, nullptr); return; }
+      if (m.kv_e4m3) kv_read_stage<T>(m, l, rw.seq0, rw.start + rw.rps);
       {
         const Grp q = group(0);                     // one launch over all sequences (grid.z)
         AttnArgs a{};
-        a.q = q.qbuf; a.out = q.attn; a.kv_pool = l.kv; a.page_table = m.page_table; a.page_size = m.page_size; a.n_pages = m.n_pages;
+        a.q = q.qbuf; a.out = q.attn; a.kv_pool = m.kv_e4m3 ? m.kv_stage : l.kv; a.page_table = m.page_table; a.page_size = m.page_size; a.n_pages = m.n_pages;
         a.row_pos = q.row_pos; a.R = rw.rps; a.H = f.n_heads; a.Hkv = f.n_kv_heads; a.cross = 0; a.kv_len = 0;
         a.scale = (f.arch == SD_ARCH_T5DEC) ? 1.0f : 1.0f / sqrtf((float)f.d_head);
         a.rel_bias = m.rel_bias; a.bucket_lut = m.bucket_lut; a.rel_buckets = f.rel_buckets;
@@ -1020,15 +1089,18 @@ void forward_rows(sd_ctx* c, Model& m, const Rows& rw, float* logits) {
       RowsGemmArgs a = normed(l.ln1g, l.ln1b);
       const int nq0 = cache_only ? m.nq : 0;         // features left out: the queries
       a.W = cb(l.wqkv) + (size_t)nq0 * d; a.bias = l.bqkv ? cb(l.bqkv) + nq0 : nullptr; a.N = m.nq + 2 * m.nkv - nq0;
-      a.q = q; a.nq = m.nq - nq0; a.nkv = m.nkv; a.kv_pool = static_cast<bf16*>(l.kv); a.page_table = m.page_table;
+      a.q = q; a.nq = m.nq - nq0; a.nkv = m.nkv; a.kv_pool = static_cast<bf16*>(m.kv_e4m3 ? m.kv_stage : l.kv); a.page_table = m.page_table;
       a.row_seq = m.row_seq; a.pt_stride = m.n_pages;
       a.row_pos = m.row_pos; a.page_size = m.page_size; a.n_kv_heads = f.n_kv_heads; a.d_head = f.d_head; a.rope = m.rope;
       launch_gemm_rows<EPI_QKV>(s, m, a);
+      if (m.kv_e4m3) kv_append_stage<bf16>(m, l, rows);
     }
     if (cache_only) break;
     auto attention = [&](bool cross) {
+      if (m.kv_e4m3 && rw.mode != ROWS_PREFILL) { kv_attention<bf16>(m, l, rw, attn); return; }
+      if (m.kv_e4m3) kv_read_stage<bf16>(m, l, rw.seq0, rw.start + rw.rps);
       AttnArgs a{};
-      a.q = q; a.out = attn; a.kv_pool = l.kv; a.page_table = m.page_table; a.page_size = m.page_size; a.n_pages = m.n_pages;
+      a.q = q; a.out = attn; a.kv_pool = m.kv_e4m3 ? m.kv_stage : l.kv; a.page_table = m.page_table; a.page_size = m.page_size; a.n_pages = m.n_pages;
       a.row_pos = m.row_pos; a.R = rw.rps; a.H = f.n_heads; a.Hkv = f.n_kv_heads;
       a.scale = (f.arch == SD_ARCH_T5DEC) ? 1.0f : 1.0f / sqrtf((float)f.d_head);
       a.bias_by_key = m.bias_by_key; a.bias_off = f.max_len - 1;
@@ -1333,7 +1405,7 @@ extern "C" size_t sd_workspace_bytes(const sd_model_cfg* p_cfg, const sd_model_c
                                      const sd_runtime_cfg* rt) {
   std::string why;
   if (!p_cfg || !q_cfg || !rt || !cfg_ok(*p_cfg, why) || !cfg_ok(*q_cfg, why) || !rt_ok(*rt, why)) return 0;
-  if (p_cfg->vocab != q_cfg->vocab) return 0;
+  if (p_cfg->vocab != q_cfg->vocab || !kv_flag_ok(*p_cfg, *rt, why)) return 0;
   return plan_bytes(*p_cfg, *q_cfg, *rt, ROWS_PASS_MAX);
 }
 
@@ -1347,6 +1419,7 @@ extern "C" sd_status sd_load_models(sd_ctx** out, const sd_model_cfg* p_cfg, con
   if (!cfg_ok(*q_cfg, why)) return fail(nullptr, SD_EINVAL, "Mq config: " + why);
   if (!rt_ok(*rt, why)) return fail(nullptr, SD_EINVAL, "runtime config: " + why);
   if (p_cfg->vocab != q_cfg->vocab) return fail(nullptr, SD_EINVAL, "Mp and Mq must share the vocabulary");
+  if (!kv_flag_ok(*p_cfg, *rt, why)) return fail(nullptr, SD_EINVAL, why);
   if (rt->batch > 1 && (p_cfg->arch == SD_ARCH_T5DEC || q_cfg->arch == SD_ARCH_T5DEC))
     return fail(nullptr, SD_EINVAL, "T5DEC models take one sequence (one encoder output per context)");
   if ((rt->max_gamma + 1) * (p_cfg->n_heads / p_cfg->n_kv_heads) > ATTN_MAX_RG ||
@@ -1406,6 +1479,10 @@ extern "C" sd_status sd_load_models(sd_ctx** out, const sd_model_cfg* p_cfg, con
   for (const Model* m : {&c->p, &c->q})
     if (m->zeros) hipLaunchKernelGGL(fill_u32_kernel, dim3(1), dim3(256), 0, c->stream, reinterpret_cast<unsigned int*>(m->zeros), 0u, (size_t)256);
   hipLaunchKernelGGL(clear_tickets_kernel, dim3(1), dim3(SD_MAX_BATCH), 0, c->stream, c->d_scratch, sizeof(SampleScratch), (int)B, SAMPLE_TICKETS);
+  if (c->p.kv_e4m3) {
+    const size_t n = B * p_cfg->n_kv_heads * KV_MODEL_GROUPS;
+    hipLaunchKernelGGL(fill_u32_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, c->stream, c->p.kv_tickets, 0u, n);
+  }
   hipError_t e = hipStreamSynchronize(c->stream);
   if (e == hipSuccess) e = hipGetLastError();
   if (e != hipSuccess) return bail(SD_EHIP, std::string("load: ") + hipGetErrorString(e));
@@ -1653,8 +1730,9 @@ extern "C" sd_status sd_debug_logits(sd_ctx* c, int32_t which, float* host_out, 
 
 extern "C" sd_status sd_set_flags(sd_ctx* c, int32_t flags) {
   if (!c) return SD_EINVAL;
-  if (flags & ~(SD_FLAG_GRAPH | SD_FLAG_PROFILE | SD_FLAG_BETA | SD_FLAG_SCATTER_PAGES | SD_FLAG_SEPARATE_CROSS_Q)) return fail(c, SD_EINVAL, "unknown flag");
-  flags = (flags & ~SD_FLAG_SCATTER_PAGES) | (c->rt.flags & SD_FLAG_SCATTER_PAGES);    // the cache layout is fixed at load
+  constexpr int at_load = SD_FLAG_SCATTER_PAGES | SD_FLAG_KV_E4M3;                     // the cache layout is fixed at load
+  if (flags & ~(SD_FLAG_GRAPH | SD_FLAG_PROFILE | SD_FLAG_BETA | SD_FLAG_SEPARATE_CROSS_Q | at_load)) return fail(c, SD_EINVAL, "unknown flag");
+  flags = (flags & ~at_load) | (c->rt.flags & at_load);
   if ((flags ^ c->rt.flags) & (SD_FLAG_BETA | SD_FLAG_SEPARATE_CROSS_Q)) {            // the captured iteration changes
     HIP_TRY(c, hipStreamSynchronize(c->stream));
     for (auto& g : c->graphs) if (g) { hipGraphExecDestroy(g); g = nullptr; }

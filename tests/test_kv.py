@@ -92,3 +92,47 @@ def test_scratch_holds_what_the_ranges_leave(n_seq, H, Hkv, R, max_len):
     per_range = 4 * n_seq * Hkv * R * (H // Hkv) * 130
     assert n - 4 * 65536 >= (-(-max_len // 4096) * per_range if max_len > 4096 else 0)
     assert n - 4 * 65536 <= 2 * min(128, -(-max_len // 128)) * per_range
+
+
+# ------------------------------------------------------------------ a target with an 8-bit cache
+from oracle import transformer as T                     # noqa: E402
+from paper_2211_17192_amd import synth                  # noqa: E402
+from test_launches import launches, pair, run           # noqa: E402, F401
+
+
+def workspace(cfg_p, cfg_q, flags, batch=1):
+    rt = b._RuntimeCfg(batch=batch, max_gamma=4, page_size=16, flags=flags)
+    return b.lib.sd_workspace_bytes(C.byref(b._cfg_struct(cfg_p)), C.byref(b._cfg_struct(cfg_q)), C.byref(rt))
+
+
+def test_an_8_bit_cache_takes_half_the_memory_and_one_layer():
+    cfg = synth.model_cfg(T.GQA, 16, 256, 8, 512, 512, 4096, n_kv_heads=8, d_head=128, dtype="bf16")
+    small = dict(cfg, n_layers=1)
+    layer = 8 * 4096 * 2 * 8 * 128                      # rows of one layer's cache, 8 sequences
+    saved = workspace(cfg, small, 0, 8) - workspace(cfg, small, b.SD_FLAG_KV_E4M3, 8)
+    exps = layer // 128
+    assert 16 * layer - 16 * exps - 2 * layer - (64 << 20) <= saved <= 16 * layer - 16 * exps - 2 * layer + (1 << 20)
+
+
+def test_targets_with_a_position_bias_have_no_8_bit_cache():
+    cfg, draft = pair(T.T5DEC, enc_len=61)
+    gqa, _ = pair(T.GQA, n_kv_heads=2)
+    assert workspace(cfg, draft, b.SD_FLAG_KV_E4M3) == 0 and workspace(cfg, draft, 0) > 0
+    assert workspace(gqa, draft, b.SD_FLAG_KV_E4M3) > 0            # (a draft may have one: its cache stays as it is)
+
+
+@pytest.mark.parametrize("arch,dtype,kw,batch", [(T.GPT, "f32", {}, 1), (T.GPT, "bf16", {}, 1), (T.GQA, "bf16", dict(n_kv_heads=2), 18)])
+def test_what_a_target_with_an_8_bit_cache_launches(run, arch, dtype, kw, batch):       # noqa: F811
+    """Each layer of a verify forward appends and attends over the 8-bit cache; a prompt's layers append and, but for the last, read back for the
+    attention of the storage type.  The draft launches what it always does."""
+    calls = [f"load {batch} 4 33 1 0", *(f"prefill {i} 100" for i in range(batch)), "time 0 4", "time 1 1"]
+    out = run(*pair(arch, dtype=dtype, **kw), *calls)
+    kinds = lambda lines: [next((k for k in ("kv_append", "kv_read", "kv_attention", "attn_mma", "attn_kernel") if k in n), None) for _, n, _, _ in launches(lines)]
+    prompt, verify, draft = (([k for k in kinds(lines) if k]) for lines in (out[1], out[-2], out[-1]))
+    assert verify == ["kv_append", "kv_attention"] * 2
+    own = "attn_mma" if dtype == "bf16" else "attn_kernel"
+    assert draft == [own]
+    per_pass = ["kv_append", "kv_read", own, "kv_append"]
+    assert prompt[:4] == per_pass and prompt.count("kv_append") == 2 * prompt.count("kv_read") and "kv_attention" not in prompt
+    calls[0] = f"load {batch} 4 1 1 0"
+    assert not any(k and k.startswith("kv_") for lines in run(*pair(arch, dtype=dtype, **kw), *calls) for k in kinds(lines))
