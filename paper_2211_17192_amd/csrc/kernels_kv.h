@@ -290,8 +290,11 @@ struct KvAttnArgs {
 
 // One pass over the keys with the running maximum and sum of the softmax; both products on the matrix cores in bf16, with exact
 // operands: codes times their power of two, bf16 queries, fp32 queries and the probabilities as sums of bf16 numbers (NQ, NP of them).
-//   S^T = K Q^T   16x16x32, A = 16 keys, B = 16 (row, head) pairs.  A lane loads 16 bytes of its key's row; which features of the row a lane
-//                 of the fragment holds is free as long as K and Q agree.  The conversion from e4m3 multiplies by the key's power of two.
+//   S^T = K Q^T   16x16x32, A = 16 keys, B = 16 (row, head) pairs.  A lane takes 16 bytes of its key's row; which features of the row a lane
+//                 of the fragment holds is free as long as K and Q agree.  The conversion from e4m3 multiplies by the key's power of two.  Loaded like
+//                 this, 16 lanes touch 16 lines, so a CU gets through fewer bytes; calls that memory bounds load whole rows and turn them in LDS, which
+//                 costs the others more than they wait (64 sequences of up to 8192, 1 row, 8 kv heads of 128: 137 us directly, 125 through LDS, in bf16 half as
+//                 many 148 and 122; 16 of 2048 15.6 and 16.1).  Rows under 128 bytes are taken directly (heads of 32 47 us, 50 through LDS).
 //   O^T = V^T P   A = 16 features x 32 keys: V's rows go through the wavefront's own part of LDS and come back transposed
 //                 (ds_read_b64_tr_b8 / _b16), B = the probabilities as the lane has them, times V's powers of two.
 // The wavefronts take turns of 32 keys, each with its own maximum, sum and output; they are joined
@@ -305,7 +308,7 @@ struct KvAttnArgs {
 // Every sum is spelled out (fmaf), so that all builds of this kernel give a row the same bits.
 // grid = (pairs of sequence and kv head x groups, ranges).  Workgroups take turns on the XCDs, so the groups of a pair, which read the same keys and
 // values at about the same time, lie eight apart: one of them comes from memory, the others find the lines in their L2.
-template <typename T, int DH, int NW, int NRT, bool E4M3> struct KvShape {
+template <typename T, int DH, int NW, int NRT, bool E4M3, bool ONCE> struct KvShape {
   static constexpr int ES = E4M3 ? 1 : 2;            // bytes of an element of the cache
   static constexpr int KT = 2;                       // key tiles of a step
   static constexpr int STEP = 16 * KT;
@@ -316,7 +319,8 @@ template <typename T, int DH, int NW, int NRT, bool E4M3> struct KvShape {
   static constexpr int RPL = 64 / PPR;               // rows of V per load of the wavefront
   static constexpr int NV = STEP / RPL;
   static constexpr int NQ = sizeof(T) == 4 ? 3 : 1, NP = sizeof(T) == 4 ? 3 : 2;
-  static constexpr int STAGE = STEP * RB;            // LDS of a wavefront
+  static constexpr bool LDS_K = (ONCE || NRT == 2) && RB >= 128;            // K goes through LDS too
+  static constexpr int STAGE = (LDS_K ? 2 : 1) * STEP * RB;                  // LDS of a wavefront: V, then K
   static constexpr int most(int a, int b) { return a > b ? a : b; }
   static constexpr int ML = KV_MAX_RANGES * KV_ROWS * NRT * 8;               // the ranges' (m, l)
   static constexpr int LDS = most(most(NW * STAGE, NW * KV_ROWS * (DH + 4) * 4), ML + 64 * NW * 16);
@@ -330,11 +334,17 @@ template <int DH, bool E4M3> __device__ __forceinline__ int kv_swizzle(int row) 
   return id / RP;                                    // (below DH / 16)
 }
 
+// ... and for K, of which lanes read the same piece of 16 rows: the pieces of a row exchanged so that those of rows next to each other differ in their banks.
+template <int DH, bool E4M3> __device__ __forceinline__ int kv_swizzle_k(int row) {
+  constexpr int PPR = DH * (E4M3 ? 1 : 2) / 16;
+  return PPR >= 8 ? row & 7 : row / (8 / PPR) & (PPR - 1);
+}
+
 template <bool ONCE, typename V> __device__ __forceinline__ V kv_load(const V* p) { return ONCE ? __builtin_nontemporal_load(p) : *p; }
 
 template <typename T, int DH, int NW, int NRT, bool E4M3, bool ONCE>
 static __global__ __launch_bounds__(64 * NW, 2) void kv_attention_kernel(const KvAttnArgs a) {
-  using S = KvShape<T, DH, NW, NRT, E4M3>;
+  using S = KvShape<T, DH, NW, NRT, E4M3, ONCE>;
   constexpr int KT = S::KT, KL = S::KL, NV = S::NV, NQ = S::NQ, NP = S::NP, STEP = S::STEP, TURN = NW * STEP, RB = S::RB, DT = DH / 16, KSQ = DH / 32;
   typedef short s16x4 __attribute__((ext_vector_type(4)));
   typedef short s16x8 __attribute__((ext_vector_type(8)));
@@ -384,8 +394,8 @@ static __global__ __launch_bounds__(64 * NW, 2) void kv_attention_kernel(const K
   // ---- loads ----
   const unsigned page_rows = 2u * (unsigned)a.c.Hkv << a.c.page_shift, v_rows = (unsigned)a.c.Hkv << a.c.page_shift;
   const unsigned slot_mask = (1u << a.c.page_shift) - 1u;
-  const int k_lane = j * RB + kq * S::FPL * S::ES;   // this lane's bytes of a key tile
-  const int vpiece = lane % S::PPR, vrow = lane / S::PPR;
+  const int k_lane = j * RB + kq * S::FPL * S::ES;   // this lane's bytes of a key tile, as the product takes them
+  const int vpiece = lane % S::PPR, vrow = lane / S::PPR;      // ... of rows loaded whole
   // first row of the pool of tile kt of step i (its K); what lies behind the end re-reads a tile that was just read (the step's first, or that of the
   // step before it), which costs no memory traffic
   auto tile_row = [&](int i, int kt, int end) -> unsigned long long {
@@ -395,33 +405,41 @@ static __global__ __launch_bounds__(64 * NW, 2) void kv_attention_kernel(const K
     return (unsigned long long)page * page_rows + ((unsigned)hkv << a.c.page_shift) + ((unsigned)(kb0 + ii * TURN + t * 16) & slot_mask);
   };
   const unsigned char* pool = static_cast<const unsigned char*>(a.c.pool);
-  u32x4 kr[KT][KL], vr[NV];
+  u32x4 kr[S::most(KT * KL, NV)], vr[NV];
   unsigned ke[KT], ve[KT];
+  auto load_rows = [&](u32x4* to, const unsigned long long (&row)[KT]) {           // RPL rows a load: within a tile of 16, or two of them
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+      constexpr int RPL = S::RPL;
+      if constexpr (RPL <= 16) to[c] = kv_load<ONCE>(reinterpret_cast<const u32x4*>(pool + (row[c * RPL / 16] + (c * RPL) % 16) * RB + vrow * RB + vpiece * 16));
+      else to[c] = kv_load<ONCE>(reinterpret_cast<const u32x4*>(pool + (vrow < 16 ? row[2 * c] : row[2 * c + 1]) * RB + (vrow & 15) * RB + vpiece * 16));
+    }
+  };
   auto load_k = [&](int i, int end) {
+    unsigned long long row[KT];
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-      const unsigned long long row = tile_row(i, kt, end);
-      const unsigned char* base = pool + row * RB;
+    for (int kt = 0; kt < KT; ++kt) row[kt] = tile_row(i, kt, end);
+    if constexpr (S::LDS_K) load_rows(kr, row);
+    else {
 #pragma unroll
-      for (int l = 0; l < KL; ++l) {
-        const unsigned char* p = base + k_lane + l * 4 * S::FPL * S::ES;
-        if constexpr (S::FPL * S::ES == 16) kr[kt][l] = kv_load<ONCE>(reinterpret_cast<const u32x4*>(p));
-        else { const u32x2 x = kv_load<ONCE>(reinterpret_cast<const u32x2*>(p)); kr[kt][l] = u32x4{x[0], x[1], 0u, 0u}; }
-      }
-      if (E4M3) ke[kt] = *(a.c.exps + row + j);
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int l = 0; l < KL; ++l) {
+          const unsigned char* p = pool + row[kt] * RB + k_lane + l * 4 * S::FPL * S::ES;
+          if constexpr (S::FPL * S::ES == 16) kr[kt * KL + l] = kv_load<ONCE>(reinterpret_cast<const u32x4*>(p));
+          else { const u32x2 x = kv_load<ONCE>(reinterpret_cast<const u32x2*>(p)); kr[kt * KL + l] = u32x4{x[0], x[1], 0u, 0u}; }
+        }
+    }
+    if (E4M3) {
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) ke[kt] = *(a.c.exps + row[kt] + j);
     }
   };
   auto load_v = [&](int i, int end) {
     unsigned long long row[KT];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) row[kt] = tile_row(i, kt, end) + v_rows;
-#pragma unroll
-    for (int c = 0; c < NV; ++c) {
-      // RPL rows a load: within a tile of 16, or two of them
-      constexpr int RPL = S::RPL;
-      if constexpr (RPL <= 16) vr[c] = kv_load<ONCE>(reinterpret_cast<const u32x4*>(pool + (row[c * RPL / 16] + (c * RPL) % 16) * RB + vrow * RB + vpiece * 16));
-      else vr[c] = kv_load<ONCE>(reinterpret_cast<const u32x4*>(pool + (vrow < 16 ? row[2 * c] : row[2 * c + 1]) * RB + (vrow & 15) * RB + vpiece * 16));
-    }
+    load_rows(vr, row);
     if (E4M3) {
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt) ve[kt] = *reinterpret_cast<const unsigned*>(a.c.exps + row[kt] + kq * 4);
@@ -461,7 +479,7 @@ static __global__ __launch_bounds__(64 * NW, 2) void kv_attention_kernel(const K
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) o[dt][rt] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  unsigned char* vt = lds + wave * S::STAGE;
+  unsigned char *vt = lds + wave * S::STAGE, *kt_lds = vt + STEP * RB;
   // where this lane's transposing reads begin: e4m3 row s / 2 of the eight keys 4 kq + {0..3, 16..19}, bf16 row s / 4 of four keys
   const int tr_row = E4M3 ? ((j >> 3) * 16 + kq * 4 + (j >> 1 & 3)) : (kq * 4 + (j >> 2));
   const int tr_at = tr_row * RB + (E4M3 ? 8 * (j & 1) : 8 * (j & 3)), tr_swz = kv_swizzle<DH, E4M3>(tr_row);
@@ -496,6 +514,14 @@ static __global__ __launch_bounds__(64 * NW, 2) void kv_attention_kernel(const K
     }
   };
 
+  auto k_to_lds = [&](const u32x4* x) {
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+      const int row = c * S::RPL + vrow;
+      *reinterpret_cast<u32x4*>(kt_lds + row * RB + (vpiece ^ kv_swizzle_k<DH, E4M3>(row)) * 16) = x[c];
+    }
+  };
+
   int far = pos[0], near = pos[0] < 0 ? 0x7fffffff : pos[0];
 #pragma unroll
   for (int rt = 1; rt < NRT; ++rt) { far = max(far, pos[rt]); near = min(near, pos[rt] < 0 ? 0x7fffffff : pos[rt]); }
@@ -508,7 +534,7 @@ static __global__ __launch_bounds__(64 * NW, 2) void kv_attention_kernel(const K
   for (int i = 0, kb = kb0; kb < end; ++i, kb += TURN) {
     const unsigned tiles_ok = (unsigned)(ok_tiles >> ((i * KT) & 63)) & ((1u << KT) - 1u);
     const bool clean = kb + STEP - 1 <= pos_min && tiles_ok == (1u << KT) - 1u;        // uniform: every row sees every key of the step
-    // ---- V into LDS; its registers take the next step's ----
+    // ---- K and V into LDS; their registers take the next step's ----
     if (!clean) {
       unsigned bad = 0;
 #pragma unroll
@@ -564,30 +590,46 @@ static __global__ __launch_bounds__(64 * NW, 2) void kv_attention_kernel(const K
       }
     }
     v_to_lds(vr);
-    unsigned vs[KT];
+    if constexpr (S::LDS_K) k_to_lds(kr);
+    unsigned ks[KT], vs[KT];
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) vs[kt] = E4M3 ? ve[kt] : 0u;
+    for (int kt = 0; kt < KT; ++kt) { ks[kt] = E4M3 ? ke[kt] : 0u; vs[kt] = E4M3 ? ve[kt] : 0u; }
     load_v(i + 1, end);
+    if constexpr (S::LDS_K) {
+      load_k(i + 1, end);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");   // this step's rows have landed in LDS
+    }
     // ---- scores: sc[kt][rt][r] = S[key kb + kt 16 + kq 4 + r][pair rt 16 + j] ----
     f32x4 sc[KT][NRT];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
+      u32x4 kx[KL];
+#pragma unroll
+      for (int l = 0; l < KL; ++l) {
+        if constexpr (!S::LDS_K) kx[l] = kr[kt * KL + l];
+        else {
+          const int row = kt * 16 + j, at = (l * 4 + kq) * S::FPL * S::ES;
+          const unsigned char* from = kt_lds + row * RB + ((at >> 4) ^ kv_swizzle_k<DH, E4M3>(row)) * 16;
+          if constexpr (S::FPL * S::ES == 16) kx[l] = *reinterpret_cast<const u32x4*>(from);
+          else { const u32x2 x = *reinterpret_cast<const u32x2*>(from + (at & 15)); kx[l] = u32x4{x[0], x[1], 0u, 0u}; }
+        }
+      }
       bf16x8 kf[KSQ];
       if constexpr (E4M3) {
-        const float s2 = __uint_as_float(ke[kt] << 23);
+        const float s2 = __uint_as_float(ks[kt] << 23);
 #pragma unroll
         for (int s = 0; s < KSQ; ++s) {
           constexpr int U = S::FPL / 8;
 #pragma unroll
           for (int w = 0; w < 2; ++w) {
-            const unsigned x = kr[kt][s / U][(s % U) * 2 + w];
+            const unsigned x = kx[s / U][(s % U) * 2 + w];
             const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, s2, false), hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, s2, true);
             kf[s][4 * w] = lo[0]; kf[s][4 * w + 1] = lo[1]; kf[s][4 * w + 2] = hi[0]; kf[s][4 * w + 3] = hi[1];
           }
         }
       } else {
 #pragma unroll
-        for (int s = 0; s < KSQ; ++s) kf[s] = __builtin_bit_cast(bf16x8, kr[kt][s]);
+        for (int s = 0; s < KSQ; ++s) kf[s] = __builtin_bit_cast(bf16x8, kx[s]);
       }
 #pragma unroll
       for (int rt = 0; rt < NRT; ++rt) {
@@ -598,7 +640,7 @@ static __global__ __launch_bounds__(64 * NW, 2) void kv_attention_kernel(const K
           for (int s = 0; s < KSQ; ++s) sc[kt][rt] = mma_bf16(kf[s], qf[rt][n][s], sc[kt][rt]);
       }
     }
-    load_k(i + 1, end);
+    if constexpr (!S::LDS_K) load_k(i + 1, end);
     // ---- softmax: the reference m_run only moves when scores outgrow it by 2^8 ----
     float f[NRT];
     bool rescale = false;
@@ -818,15 +860,15 @@ constexpr size_t KV_TICKET_BYTES = (size_t)KV_TICKETS * sizeof(unsigned);
 
 // How a call is cut into workgroups.  `pairs`: (row, query head) pairs of a kv head.  Measured in graphs over three sets of inputs, us a call; 8 kv heads
 // of 128 in e4m3 and 4 query heads each unless said.
-//   Calls over 128 MB of keys and values or more are bound by memory: loads past the L2s where one workgroup reads a line (64 sequences of 8192, one row 198 -> 181; what
-//   several groups read is left in them: two groups 240 -> 340), and two tiles of pairs a workgroup (64 of 8192, 5 rows 242 -> 191, 64 of 2048 70 -> 53).  Below
+//   Calls over 128 MB of keys and values or more are bound by memory: loads past the L2s where one workgroup reads a line (64 sequences of 8192, one row 198 -> 184; what
+//   several groups read is left in them: two groups of two tiles 335 -> 350), and two tiles of pairs a workgroup (64 of 8192, 5 rows 298 -> 200, 64 of 2048 81 -> 56).  Below
 //   that one tile and more workgroups (16 of 2048, 5 rows 16.3 against 22; one of 500 7.8 against 10.5), and plain loads (16 of 2048, one row 15.3 against 17.3: the
 //   memory-side cache holds them from call to call).  fp32 queries have no registers for two tiles.
 //   Ranges: where there are fewer workgroups than CUs, as many as fill those; not for short contexts, where the join (2.6 us) costs more than the steps that it saves
 //   (one sequence of 500 7.2 against 8.4 in two ranges, of 1000 10.4 against 8.4 in four; heads of 64 are half the work: 1000 7.2 against 8.1), and 16 of 2048 are better
 //   in one range (15.3, 16.8 in two); nor more than the join is worth (one of 8192 in 8, 16, 32 ranges 13.9, 11.7, 13.3; of 32768 in 16, 32, 64 20.9, 19.0, 23.9).
-//   At most 4096 keys (64 of 8192 in ranges of 1024, 2048, 4096 207, 192, 181; contexts between a quarter of that and all of it 143, 140, 144).
-//   Eight wavefronts where a CU has one workgroup of 512 keys or more (16 of 2048 15.3, 17.3 with four; 64 of 2048 53.9, 52.3), unless they are few (one of 1000 9.7, 8.4).
+//   At most 4096 keys (64 of 8192 in ranges of 1024, 2048, 4096 199, 180, 176; contexts of all lengths up to that 127, 123, 125).
+//   Eight wavefronts where a CU has one workgroup of 512 keys or more (16 of 2048 15.3, 17.3 with four; 64 of 2048 56.8, 52.6), unless they are few (one of 1000 9.7, 8.4).
 struct KvPlan { int rows_wg, groups, range_keys, n_ranges, waves; bool large, once; };
 // What the sums of a row depend on: the ranges and the wavefronts.  wgs: (sequence, kv head, group)s.
 inline void kv_plan_ranges(KvPlan& p, long long wgs, long long heads, int max_len, int d_head, bool e4m3) {

@@ -298,6 +298,25 @@ def test_attention_cut_for_long_contexts(dtype, cache_dtype, S, H, Hkv, R):
 
 @pytest.mark.parametrize("cache_dtype", ["e4m3", "bf16"])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,page", [(32, 16), (64, 16), (64, 64)])
+@pytest.mark.parametrize("R", [1, 5])
+def test_small_heads_cut_for_long_contexts(dtype, cache_dtype, D, page, R):
+    """Rows of 32, 64 and 128 bytes in calls whose contexts may be 60000 long: one tile and two."""
+    S, H, Hkv, max_len = 5, 32, 8, 60000
+    lens = [700, 33, 5, 1000, 257]
+    cache, g = make(S, 1024 // page, Hkv, D, page, cache_dtype, 22)
+    plain = fill(cache, g, lens, dtype=dtype)
+    wide = torch.zeros(S, -(-max_len // page), dtype=torch.int32, device="cuda")
+    wide[:, :1024 // page] = cache.page_table
+    cache = type(cache)(wide, cache.pool.shape[0], Hkv, D, page_size=page, dtype=cache_dtype, pool=cache.pool, exps=cache.exps)
+    q = normal(g, S, R, H, D, dtype=dtype, std=2.0)
+    pos = torch.tensor([[L - R + r for r in range(R)] for L in lens], dtype=torch.int32, device="cuda")
+    lse = torch.empty(S, R, H, device="cuda")
+    check_attention(cache.attention(q, pos, max_len=max_len, lse=lse), lse, q, plain, pos)
+
+
+@pytest.mark.parametrize("cache_dtype", ["e4m3", "bf16"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("H,Hkv,D,R,max_len", [(32, 8, 128, 1, 700), (32, 8, 128, 5, 2600), (64, 32, 64, 1, 1200), (16, 16, 32, 3, 3000)])
 def test_attention_with_eight_wavefronts(dtype, cache_dtype, H, Hkv, D, R, max_len):
     lens = [700, 512, 257, 256, 255, 1, 33, 600]
