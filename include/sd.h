@@ -470,7 +470,7 @@ typedef struct {
  * Write rows into the cache / read rows of it.
  *   seq, pos : dev, [rows] int32: row i is position pos[i] of sequence seq[i].  seq == NULL: every sequence has
  *              rows / n_seq rows, one after the other.  pos == NULL: positions 0, 1, .. of each sequence.
- *   rows     : 0 is allowed and does nothing
+ *   rows     : 0 is allowed and does nothing; K's (or V's) rows of a call are less than 2^36 bytes (SD_ERANGE)
  * A row whose position is negative or beyond the table, whose sequence is none of the n_seq, or whose table entry has no
  * page is not written, and read as zeros.  Two rows of one append at the same place: what the
  * cache then holds there is unspecified.  In an SD_BF16 cache values are rounded to bf16.

@@ -37,9 +37,10 @@ sd_status kv_rows(const sd_kv_cache* cache, const sd_kv_rows* x, const int32_t* 
   if (st != SD_OK) return st;
   if (rows < 0) return kv_fail(SD_EINVAL, "negative number of rows");
   if (rows == 0) return SD_OK;
-  if (((int64_t)rows / 8 + 1) * cache->n_kv_heads > 0x7fffffff) return kv_fail(SD_ERANGE, "too many rows");
   if (!x || !x->k || !x->v) return kv_fail(SD_EINVAL, "null rows");
   if (x->dtype != SD_F32 && x->dtype != SD_BF16) return kv_fail(SD_EINVAL, "rows are SD_F32 or SD_BF16");
+  const int64_t block_rows = sd::KV_ROW_BYTES / (cache->d_head * (x->dtype == SD_F32 ? 4 : 2));
+  if (((int64_t)rows + block_rows - 1) / block_rows * cache->n_kv_heads >= 1 << 24) return kv_fail(SD_ERANGE, "too many rows");      // 2^32 threads
   if (!aligned16(x->k) || !aligned16(x->v)) return kv_fail(SD_EINVAL, "rows must be 16-byte aligned");
   if ((x->k_row_stride | x->k_head_stride | x->v_row_stride | x->v_head_stride) & 7) return kv_fail(SD_EINVAL, "strides must be multiples of 8 elements");
   if (!seq && rows % cache->n_seq) return kv_fail(SD_EINVAL, "without seq every sequence has the same number of rows");
@@ -62,7 +63,7 @@ sd_status kv_attention_plan(const sd_kv_cache* c, int32_t n_heads, int32_t rows,
   const int64_t pairs = (int64_t)rows * (n_heads / c->n_kv_heads);
   if (pairs > 65535 || (int64_t)c->n_seq * rows * n_heads > 0x7fffffff / 128) return kv_fail(SD_ERANGE, "too many rows");
   p = sd::kv_plan(c->n_seq, c->n_kv_heads, (int)pairs, max_len, c->d_head, c->dtype == SD_E4M3, dtype == SD_F32);
-  if ((int64_t)c->n_seq * c->n_kv_heads * p.groups > SD_KV_MAX_GROUPS || (int64_t)p.groups * p.n_ranges > 65535)
+  if ((int64_t)c->n_seq * c->n_kv_heads * p.groups > SD_KV_MAX_GROUPS)
     return kv_fail(SD_ERANGE, "more than SD_KV_MAX_GROUPS (sequence, 16 rows, kv head)s");
   return SD_OK;
 }
@@ -100,13 +101,13 @@ extern "C" sd_status sd_kv_attention(const sd_kv_cache* cache, const void* q, in
   if (!q || !pos || !out || !scratch) return kv_fail(SD_EINVAL, "null pointer");
   if (!aligned16(q) || !aligned16(out) || !aligned16(scratch)) return kv_fail(SD_EINVAL, "q, out and scratch must be 16-byte aligned");
   if ((q_row_stride | q_head_stride) & 7) return kv_fail(SD_EINVAL, "strides must be multiples of 8 elements");
-  if (!(scale > 0.0f) || !std::isfinite(scale)) return kv_fail(SD_EINVAL, "scale must be positive");
+  a.c_log2 = scale * 1.44269504088896340736f;
+  if (!(scale > 0.0f) || !std::isfinite(a.c_log2)) return kv_fail(SD_EINVAL, "scale must be positive");
   if (scratch_bytes < sd::kv_scratch_bytes(cache->n_seq, cache->n_kv_heads, cache->d_head, p)) return kv_fail(SD_ENOMEM, "scratch too small: see sd_kv_attention_scratch_bytes");
   a.q = q; a.q_row = q_row_stride; a.q_head = q_head_stride; a.out = out; a.lse = lse; a.pos = pos;
   a.R = rows; a.H = n_heads; a.G = n_heads / cache->n_kv_heads;
   a.n_seq = cache->n_seq; a.max_len = max_len;
   sd::kv_set_plan(a, p);
-  a.c_log2 = scale * 1.44269504088896340736f;
   a.tickets = static_cast<unsigned*>(scratch);
   a.partial = reinterpret_cast<float*>(static_cast<char*>(scratch) + sd::KV_TICKET_BYTES);
   hipStream_t s = static_cast<hipStream_t>(stream);

@@ -343,6 +343,22 @@ def test_attention_over_a_very_long_context(cache_dtype, n):
     check_attention(cache.attention(q, at, max_len=n, lse=lse), lse, q, plain, at)
 
 
+def test_many_rows_cut_for_the_longest_contexts():
+    """520 groups of rows times 128 ranges of keys."""
+    from paper_2211_17192_amd import binding
+    n, R = 300, 4160
+    cache, g = make(1, 32, 1, 128, 16, "e4m3", 23)
+    plain = fill(cache, g, [n])
+    wide = torch.zeros(1, binding.SD_KV_MAX_LEN // 16, dtype=torch.int32, device="cuda")
+    wide[:, :32] = cache.page_table
+    cache = type(cache)(wide, cache.pool.shape[0], 1, 128, pool=cache.pool, exps=cache.exps)
+    q = normal(g, 1, R, 4, 128, std=2.0)
+    pos = torch.randint(-1, n, (1, R), dtype=torch.int32, device="cuda", generator=g)
+    lse = torch.empty(1, R, 4, device="cuda")
+    out = cache.attention(q, pos, max_len=binding.SD_KV_MAX_LEN, lse=lse)
+    check_attention(out, lse, q, plain, pos)
+
+
 @pytest.mark.parametrize("scale", [0.01, 1.0, 20.0])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attention_with_flat_and_peaked_weights(scale, dtype):

@@ -84,6 +84,19 @@ def test_sizes_out_of_range():
     refused(b.SD_ERANGE, "SD_KV_MAX_GROUPS", b.lib.sd_kv_attention(C.byref(cache(n_seq=9000)), AT, 4096, 128, b.SD_BF16, AT, 8, 1, 100, 0.1, AT, None, AT, 1 << 30, None))
 
 
+def test_the_largest_calls_are_told_from_those_beyond():
+    """A launch has less than 2^32 threads: 2^24 workgroups of 4096 bytes of rows.  """
+    for dtype, d, heads in ((b.SD_BF16, 128, 8), (b.SD_F32, 32, 64), (b.SD_F32, 128, 2)):
+        row = d * (2 if dtype == b.SD_BF16 else 4)
+        most = ((1 << 24) // heads - 1) * (4096 // row)
+        c, r = cache(n_kv_heads=heads, d_head=d, n_seq=1), rows(dtype=dtype)
+        refused(b.SD_ERANGE, "too many", b.lib.sd_kv_append(C.byref(c), C.byref(r), None, AT, most + 1, None))
+        refused(b.SD_ERANGE, "too many", b.lib.sd_kv_read(C.byref(c), C.byref(r), None, AT, most + 1, None))
+    refused(b.SD_EINVAL, "scale", b.lib.sd_kv_attention(C.byref(cache()), AT, 4096, 128, b.SD_BF16, AT, 32, 1, 400, 3e38, AT, None, AT, 1 << 30, None))
+    # many groups of rows times many ranges of a long context
+    assert b.lib.sd_kv_attention_scratch_bytes(C.byref(cache(n_seq=1, n_kv_heads=1)), 4, 4160, b.SD_KV_MAX_LEN) >= 520 * 128 * 32 * 130 * 4
+
+
 @pytest.mark.parametrize("n_seq,H,Hkv,R,max_len", [(1, 8, 8, 1, 1), (1, 32, 8, 1, 131072), (1, 32, 8, 16, b.SD_KV_MAX_LEN), (64, 32, 8, 5, 8192), (300, 64, 64, 1, 5000), (3, 40, 1, 7, 257)])
 def test_scratch_holds_what_the_ranges_leave(n_seq, H, Hkv, R, max_len):
     """Tickets, and per (sequence, group of up to 32 rows, kv head) and range of at most 4096 keys d_head + 2 floats a row."""
