@@ -236,13 +236,17 @@ class KvCache:
         dtype = _ROW_TYPES.get(k.dtype)
         if dtype is None or k.dtype != v.dtype:
             _refuse("k and v must be float32 or bfloat16, both the same")
-        strides = []
-        for t in (k, v):
-            shape = t.shape
-            if len(shape) < 3 or shape[-2] != self.n_kv_heads or shape[-1] != self.d_head or t.numel() != n * self._row_size:
-                _refuse(f"k and v must be [.., {self.n_kv_heads}, {self.d_head}] with a row for each of the {n} positions")
-            strides += _row_strides(shape, t.stride()) if n else (0, 0)
-        return _KvRows(k.data_ptr(), v.data_ptr(), *strides, dtype), n
+        shape, stride = k.shape, k.stride()
+        row, head = self._row_strides(shape, stride, n)
+        if v.shape == shape and v.stride() == stride:
+            return _KvRows(k.data_ptr(), v.data_ptr(), row, head, row, head, dtype), n
+        v_row, v_head = self._row_strides(v.shape, v.stride(), n)
+        return _KvRows(k.data_ptr(), v.data_ptr(), row, head, v_row, v_head, dtype), n
+
+    def _row_strides(self, shape, stride, n):
+        if len(shape) < 3 or shape[-2] != self.n_kv_heads or shape[-1] != self.d_head or shape.numel() != n * self._row_size:
+            _refuse(f"k and v must be [.., {self.n_kv_heads}, {self.d_head}] with a row for each of the {n} positions")
+        return _row_strides(shape, stride) if n else (0, 0)
 
     def append(self, k, v, pos, seq=None):
         """sd_kv_append: rows k, v [n_seq, rows, n_kv_heads, d_head] (with seq: [rows, ..]), float32 or bfloat16, to the
