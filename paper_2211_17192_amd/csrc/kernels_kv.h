@@ -867,26 +867,32 @@ constexpr size_t KV_TICKET_BYTES = (size_t)KV_TICKETS * sizeof(unsigned);
 //   Calls over 128 MB of keys and values or more are bound by memory: loads past the L2s where one workgroup reads a line (64 sequences of 8192, one row 198 -> 184; what
 //   several groups read is left in them: two groups of two tiles 335 -> 350), and two tiles of pairs a workgroup (64 of 8192, 5 rows 298 -> 200, 64 of 2048 81 -> 56).  Below
 //   that one tile and more workgroups (16 of 2048, 5 rows 16.3 against 22; one of 500 7.8 against 10.5), and plain loads (16 of 2048, one row 15.3 against 17.3: the
-//   memory-side cache holds them from call to call).  fp32 queries have no registers for two tiles.
-//   Ranges: where there are fewer workgroups than CUs, as many as fill those; not for short contexts, where the join (2.6 us) costs more than the steps that it saves
-//   (one sequence of 500 7.2 against 8.4 in two ranges, of 1000 10.4 against 8.4 in four; heads of 64 are half the work: 1000 7.2 against 8.1), and 16 of 2048 are better
-//   in one range (15.3, 16.8 in two); nor more than the join is worth (one of 8192 in 8, 16, 32 ranges 13.9, 11.7, 13.3; of 32768 in 16, 32, 64 20.9, 19.0, 23.9).
-//   At most 4096 keys (64 of 8192 in ranges of 1024, 2048, 4096 199, 180, 176; contexts of all lengths up to that 127, 123, 125).
-//   Eight wavefronts where a CU has one workgroup of 512 keys or more (16 of 2048 15.3, 17.3 with four; 64 of 2048 56.8, 52.6), unless they are few (one of 1000 9.7, 8.4).
+//   memory-side cache holds them from call to call).   In bf16 caches of heads of 128 also below it, where the
+//   groups of one tile are more than the CUs (18 of 1000 25.2 -> 17.9, 60 of 200 19.4 -> 15.3, 30 of 500 16.6 -> 15.9; in e4m3 17.3 -> 16.3, 24.1 -> 25.3, 22.3 -> 22.9).  fp32 queries have no
+//   registers for two tiles.
+//   Ranges: where there are fewer workgroups than CUs, as many as fill those, or twice as many where a row is under 128 bytes (2 sequences of 108567, 2 heads of 32
+//   24.1 -> 16.7; 4 of 6874, 12 of 64 14.7 -> 13.5; with rows of 128 bytes 4 of 8192 20.8 -> 21.7).  Not for short contexts, where the join (2.6 us for heads of 128) costs more than
+//   the steps that it saves: a step takes 0.9 us for heads of 128, 0.69 for 64, 0.56 for 32 (one sequence of 500 7.2 against 8.4 in two ranges, of 1000 10.4 against 8.4 in
+//   four; 12 heads of 64: 1500 11.2 against 8.4 in six; 2 of 32: 1000 7.8 against 7.4, 3000 16.7 against 7.3 in twelve), later where eight wavefronts can take them (16 of 2048 15.3,
+//   16.8 in two; one of 1200 with 64 heads of 64 8.7, 9.2 in five); nor more than the join is worth, which is the less the shorter the rows (one of 8192 in 8, 16, 32 ranges 13.9, 11.7,
+//   13.3; of 32768 in 16, 32, 64 20.9, 19.0, 23.9; 2 heads of 32, 16384 in 16, 43, 64 10.7, 9.0, 9.0).  At most 4096 keys (64 of 8192 in ranges of 1024, 2048, 4096 199, 180, 176;
+//   contexts of all lengths up to that 127, 123, 125).
+//   Eight wavefronts where a CU has one workgroup of 512 keys or more (16 of 2048 15.3, 17.3 with four; 64 of 1200 with 2 heads of 32 7.9, 9.2; 64 of 2048 56.8, 52.6), unless they are few
+//   (one of 1000 9.7, 8.4).
 struct KvPlan { int rows_wg, groups, range_keys, n_ranges, waves; bool large, once; };
 // What the sums of a row depend on: the ranges and the wavefronts.  wgs: (sequence, kv head, group)s.
 inline void kv_plan_ranges(KvPlan& p, long long wgs, long long heads, int max_len, int d_head, bool e4m3) {
   p.large = heads * max_len * 2 * d_head * (e4m3 ? 1 : 2) >= 128ll << 20;
   const long long per_cu = wgs < 256 ? 256 / wgs : 1;
-  const long long work = (long long)max_len * d_head / 128;                    // keys, by what a step over them takes
   long long ranges = 1;
   if (p.large) ranges = per_cu;
-  else if (work >= (per_cu > 2 ? 768 : 2560)) {
-    ranges = per_cu < (work + 255) / 256 ? per_cu : (work + 255) / 256;
-    while (ranges > 1 && 100 * ranges * ranges > 3 * work) --ranges;
+  else if (wgs < 64 ? (long long)max_len * (d_head + 128) >= 768 * 256 : (long long)max_len * d_head >= (per_cu > 2 ? 768 : 2560) * 128) {
+    const long long most = per_cu > 2 && d_head * (e4m3 ? 1 : 2) < 128 ? 512 / wgs : per_cu, parts = (max_len + 255) / 256;
+    ranges = most < parts ? most : parts;
+    while (ranges > 1 && 100 * ranges * ranges * d_head > 3 * 128 * (long long)max_len) --ranges;
   }
   long long keys = (max_len + ranges - 1) / ranges;
-  p.waves = (!p.large && wgs >= 64 && wgs <= 256 && keys * d_head / 128 >= 512) ? 8 : 4;
+  p.waves = (!p.large && wgs >= 64 && wgs <= 256 && keys >= 512 && p.rows_wg <= KV_ROWS) ? 8 : 4;
   const long long unit = 32 * p.waves, least = ((long long)max_len + KV_MAX_RANGES - 1) / KV_MAX_RANGES, longest = KV_MAX_RANGE_KEYS;
   if (keys > longest) keys = longest;
   if (keys < least) keys = least;
@@ -896,7 +902,8 @@ inline void kv_plan_ranges(KvPlan& p, long long wgs, long long heads, int max_le
 // What they do not depend on: how the rows are grouped.
 inline void kv_plan_rows(KvPlan& p, long long heads, int pairs, int max_len, int d_head, bool e4m3, bool f32) {
   p.large = heads * max_len * 2 * d_head * (e4m3 ? 1 : 2) >= 128ll << 20;
-  const int most = (p.large && !f32) ? 2 * KV_ROWS : KV_ROWS;
+  const bool many = heads * ((pairs + KV_ROWS - 1) / KV_ROWS) > 256 && !e4m3 && d_head == 128;
+  const int most = ((p.large || many) && !f32) ? 2 * KV_ROWS : KV_ROWS;
   p.groups = (pairs + most - 1) / most;
   p.rows_wg = (pairs + p.groups - 1) / p.groups;
   p.once = p.large && p.groups == 1;

@@ -343,6 +343,24 @@ def test_attention_over_a_very_long_context(cache_dtype, n):
     check_attention(cache.attention(q, at, max_len=n, lse=lse), lse, q, plain, at)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cache_dtype", ["e4m3", "bf16"])
+@pytest.mark.parametrize("S,H,Hkv,D,R,top", [(33, 32, 8, 128, 5, 90), (20, 16, 4, 128, 13, 200), (2, 4, 2, 32, 1, 9000), (3, 12, 12, 64, 6, 2100), (40, 4, 2, 32, 2, 1300)])
+def test_attention_with_many_groups_and_many_ranges(dtype, cache_dtype, S, H, Hkv, D, R, top):
+    """More groups of rows than CUs; short rows in many ranges, or with eight wavefronts."""
+    g = torch.Generator().manual_seed(24)
+    lens = [int(n) for n in torch.randint(1, top + 1, (S,), generator=g)]
+    lens[0] = top
+    cache, g = make(S, -(-top // 16), Hkv, D, 16, cache_dtype, 24)
+    plain = fill(cache, g, lens, dtype=dtype)
+    q = normal(g, S, R, H, D, dtype=dtype, std=2.0)
+    pos = torch.tensor([[L - R + r for r in range(R)] for L in lens], dtype=torch.int32, device="cuda")
+    lse = torch.empty(S, R, H, device="cuda")
+    out = cache.attention(q, pos, max_len=top, lse=lse)
+    check_attention(out, lse, q, plain, pos)
+    assert torch.equal(out, cache.attention(q, pos, max_len=top))
+
+
 def test_many_rows_cut_for_the_longest_contexts():
     """520 groups of rows times 128 ranges of keys."""
     from paper_2211_17192_amd import binding
