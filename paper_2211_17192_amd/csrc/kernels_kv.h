@@ -156,8 +156,9 @@ template <> struct KvRaw<bf16> {
   }
 };
 
-// Stores of PAST kernels go past the L2s too: where a call writes more than they hold.  (us, plain / past: 134 MB read from an e4m3 cache into bf16 rows
-// 41.3 / 25.4; into a bf16 cache 51.0 / 47.3, into an e4m3 one 41.4 / 40.9.)
+// Calls that write 8 MB or more (PAST; in a model's prompt, whose attention reads it next, what the L2s cannot hold): their stores go past the L2s too, and an append waits for a row's place before it asks for the row, so that rows which are absent
+// cost nothing; in smaller calls that wait would be seen.  (us, not / PAST: 134 MB read from an e4m3 cache into bf16 rows 41.3 / 25.4; 16 x 2047 rows of 8 heads of 128 into one 40.4 / 39.2,
+// with 3 of 8 absent 36.6 / 27.3; 8 x 700 9.7 / 8.9, 8.4 / 6.8; 2 x 1200, 5 MB, 5.0 / 5.3; into a bf16 cache 16 x 2047 51.0 / 48.8.)
 template <bool PAST, typename V> __device__ __forceinline__ void kv_store(V* p, const V& v) {
   if (PAST) __builtin_nontemporal_store(v, p);
   else *p = v;
@@ -165,7 +166,7 @@ template <bool PAST, typename V> __device__ __forceinline__ void kv_store(V* p, 
 
 // Rows in and out: 16 bytes of the rows' side of K and of V per thread, so that a wavefront's accesses are whole lines (fp32 rows by 32 bytes a thread: 131 us for
 // 268 MB read into them past the L2s, 85 through them), a workgroup per KV_ROW_BYTES / row rows of one head.  A workgroup's neighbours take the other heads of its rows.
-// Many rows are bound by memory (16 x 2047 rows of 8 heads of 128 in bf16: in 39.6 us, 5.1 TB/s as a copy; out 24.9), few by the chain position - page - row (80 rows 3.2 us).
+// Many rows are bound by memory (16 x 2047 rows of 8 heads of 128 in bf16: in 39.2 us, 5.1 TB/s as a copy; out 24.9), few by the chain position - page - row (80 rows 3.2 us).
 constexpr int KV_ROW_BYTES = 256 * 16;
 __device__ __forceinline__ void kv_rows_block(const KvRowsArgs& a, int& block, int& head) {
   block = (int)(blockIdx.x / (unsigned)a.c.Hkv);
@@ -181,12 +182,13 @@ static __global__ __launch_bounds__(256) void kv_append_kernel(const KvRowsArgs 
   const long long apart = (long long)a.c.Hkv << a.c.page_shift;                // rows of the pool from K to V
   const long long head_row = (long long)head << a.c.page_shift;
   long long place = 0;
-  if (a.paged) place = kv_place(a, ic);              // (then the rows come from such places themselves)
+  if (a.paged || PAST) place = kv_place(a, ic);      // (paged: the rows come from such places themselves)
+  if (PAST && place < 0) return;                     // (all lanes of the row)
   const long long from = (max(place, 0ll) + head_row) * DH;
   KvRaw<T> x[2];
   x[0].load(static_cast<const T*>(a.k) + (a.paged ? from : ic * a.k_row + head * a.k_head) + piece * EPT);
   x[1].load(static_cast<const T*>(a.v) + (a.paged ? from + apart * DH : ic * a.v_row + head * a.v_head) + piece * EPT);
-  if (!a.paged) place = kv_place(a, ic);
+  if (!a.paged && !PAST) place = kv_place(a, ic);
   const bool there = i < a.rows && place >= 0;
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
@@ -938,7 +940,7 @@ template <typename T> void launch_kv_rows(hipStream_t s, const KvRowsArgs& a, in
       else hipLaunchKernelGGL((kv_read_kernel<T, DH, false, P>), grid, dim3(256), 0, s, a);
     };
     const size_t written = (size_t)a.rows * a.c.Hkv * 2 * DH * (append ? (e4m3 ? 1 : 2) : sizeof(T));
-    if (written >= (size_t)32 << 20) launch(std::true_type());                 // (the eight L2s hold 4 MB each)
+    if (written >= (size_t)(a.paged ? 32 : 8) << 20) launch(std::true_type());
     else launch(std::false_type());
   });
 }

@@ -166,6 +166,33 @@ def test_rows_in_and_out(dtype, cache_dtype, H, D, page):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cache_dtype", ["e4m3", "bf16"])
+@pytest.mark.parametrize("S,R,H,D", [(3, 1500, 8, 128), (5, 3001, 12, 64), (2, 9000, 9, 32), (16, 2001, 8, 128)])
+def test_many_rows_are_what_few_at_a_time_are(dtype, cache_dtype, S, R, H, D):
+    """Padded batches of 8 MB and more against pieces of 100 rows, which the tests above pin: the whole pool, and what is read of it."""
+    from paper_2211_17192_amd import binding
+    cache, g = make(S, -(-R // 64), H, D, 64, cache_dtype, 25)
+    other = binding.KvCache(cache.page_table, cache.pool.shape[0], H, D, page_size=64, dtype=cache_dtype, pool=cache.pool.clone(), exps=None if cache.exps is None else cache.exps.clone())
+    x = normal(g, S, R, 2, H, D, dtype=dtype)
+    k, v = x[:, :, 0], x[:, :, 1]
+    pos = torch.arange(R, dtype=torch.int32, device="cuda").repeat(S, 1).contiguous()
+    for s in range(S):
+        pos[s, R - R * s // S:] = -1                   # shorter sequences
+    pos[0, ::7] = -1
+    cache.append(k, v, pos)
+    for r in range(0, R, 100):
+        other.append(k[:, r:r + 100].contiguous(), v[:, r:r + 100].contiguous(), pos[:, r:r + 100].contiguous())
+    assert torch.equal(cache.pool.view(torch.uint8), other.pool.view(torch.uint8))
+    if cache.exps is not None:
+        assert torch.equal(cache.exps, other.exps)
+    got = cache.read(pos, dtype=TYPES[dtype])
+    for r in range(0, R, 700):
+        few = other.read(pos[:, r:r + 100].contiguous(), dtype=TYPES[dtype])
+        for a, b in zip(got, few):
+            assert torch.equal(a[:, r:r + 100], b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_every_magnitude_and_tie(dtype):
     """Rows of every binade, with ties, the largest finite numbers, subnormals, zeros of both signs."""
     cache, g = make(1, 40, 1, 32, 16, "e4m3", 2)
