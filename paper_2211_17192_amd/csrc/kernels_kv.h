@@ -879,9 +879,11 @@ constexpr size_t KV_TICKET_BYTES = (size_t)KV_TICKETS * sizeof(unsigned);
 //   16.8 in two; one of 1200 with 64 heads of 64 8.7, 9.2 in five); nor more than the join is worth, which is the less the shorter the rows (one of 8192 in 8, 16, 32 ranges 13.9, 11.7,
 //   13.3; of 32768 in 16, 32, 64 20.9, 19.0, 23.9; 2 heads of 32, 16384 in 16, 43, 64 10.7, 9.0, 9.0).  At most 4096 keys (64 of 8192 in ranges of 1024, 2048, 4096 199, 180, 176;
 //   contexts of all lengths up to that 127, 123, 125).
-//   Eight wavefronts where a CU has one workgroup of 512 keys or more (16 of 2048 15.3, 17.3 with four; 64 of 1200 with 2 heads of 32 7.9, 9.2; 64 of 2048 56.8, 52.6), unless they are few
-//   (one of 1000 9.7, 8.4).
+//   Eight wavefronts for 512 keys or more where a CU has at most one workgroup (16 of 2048 15.3, 17.3 with four; 64 of 1200 with 2 heads of 32 7.9, 9.2; 64 of 2048 56.8, 52.6), and where
+//   workgroups are few only for contexts in one range (one of 700 8.3, 8.8, with 12 heads of 64 6.7, 7.4; 4 of 8192 18.7, 17.6), and of
+//   bf16 caches only for heads of 32 (16 of 1000 15.9, 14.4; 8 of 1000 with 12 heads of 64 9.6, 9.3; 64 of 2000 with 2 of 32 9.5, 11.3).
 struct KvPlan { int rows_wg, groups, range_keys, n_ranges, waves; bool large, once; };
+constexpr bool kv_eight_waves(int d_head, bool e4m3) { return e4m3 || d_head == 32; }
 // What the sums of a row depend on: the ranges and the wavefronts.  wgs: (sequence, kv head, group)s.
 inline void kv_plan_ranges(KvPlan& p, long long wgs, long long heads, int max_len, int d_head, bool e4m3) {
   p.large = heads * max_len * 2 * d_head * (e4m3 ? 1 : 2) >= 128ll << 20;
@@ -894,7 +896,7 @@ inline void kv_plan_ranges(KvPlan& p, long long wgs, long long heads, int max_le
     while (ranges > 1 && 100 * ranges * ranges * d_head > 3 * 128 * (long long)max_len) --ranges;
   }
   long long keys = (max_len + ranges - 1) / ranges;
-  p.waves = (!p.large && wgs >= 64 && wgs <= 256 && keys >= 512 && p.rows_wg <= KV_ROWS) ? 8 : 4;
+  p.waves = (kv_eight_waves(d_head, e4m3) && !p.large && wgs <= 256 && (wgs >= 64 || ranges == 1) && keys >= 512 && p.rows_wg <= KV_ROWS) ? 8 : 4;
   const long long unit = 32 * p.waves, least = ((long long)max_len + KV_MAX_RANGES - 1) / KV_MAX_RANGES, longest = KV_MAX_RANGE_KEYS;
   if (keys > longest) keys = longest;
   if (keys < least) keys = least;
@@ -958,8 +960,10 @@ template <typename T> void launch_kv_attention(hipStream_t s, const KvAttnArgs& 
     const auto one = std::integral_constant<int, 1>();
     const auto two = std::integral_constant<int, 2>();
     auto with_cache = [&](auto codes) {
-      if (p.waves == 8) launch(std::integral_constant<int, 8>(), one, codes, std::false_type());
-      else if (p.rows_wg <= KV_ROWS) {
+      if constexpr (kv_eight_waves(DH, decltype(codes)::value)) {
+        if (p.waves == 8) { launch(std::integral_constant<int, 8>(), one, codes, std::false_type()); return; }
+      }
+      if (p.rows_wg <= KV_ROWS) {
         if (p.once) launch(std::integral_constant<int, 4>(), one, codes, std::true_type());
         else launch(std::integral_constant<int, 4>(), one, codes, std::false_type());
       } else if constexpr (sizeof(T) == 2) {         // (fp32 queries: one tile)
