@@ -38,6 +38,7 @@ def _ptr(t):
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)    # (without asking whether the runtime is up)
 
 
 def _stream():
@@ -218,7 +219,7 @@ class KvCache:
         for t in tensors:
             if t is not None and t.get_device() != dev:
                 _refuse(f"a tensor lies on {t.device}, the cache on cuda:{dev}")
-        if torch.cuda.current_device() != dev:
+        if _current_device() != dev:
             _refuse(f"the cache lies on cuda:{dev}, which is not the current device")
         return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(dev)
 
@@ -283,7 +284,7 @@ class KvCache:
         if len(shape) != 4 or shape[0] != self.n_seq or shape[3] != self.d_head or dtype is None:
             _refuse(f"q must be a float32 or bfloat16 tensor [{self.n_seq}, rows, n_heads, {self.d_head}]")
         S, R, H, D = shape
-        if pos.shape != (S, R) or pos.dtype != torch.int32 or not pos.is_contiguous():
+        if pos.shape != shape[:2] or pos.dtype != torch.int32 or not pos.is_contiguous():
             _refuse("pos must be a contiguous int32 tensor [n_seq, rows]")
         if out is None:
             out = torch.empty(S, R, H, D, dtype=q.dtype, device=self._device)
